@@ -57,8 +57,10 @@ typedef struct dresd_index dresd_index; /* opaque, library-owned */
 typedef struct dresd_ivf dresd_ivf;     /* opaque: partitioned index */
 typedef void *dresd_stream;             /* a hipStream_t */
 
-/* Storage type of the keys.  Queries are always fp32; scores are fp32. */
-typedef enum { DRESD_F32 = 0, DRESD_F16 = 1, DRESD_BF16 = 2 } dresd_dtype;
+/* Storage type of the keys.  Queries are always fp32; scores are fp32.
+ * DRESD_F8 (e4m3, no infinities, largest value 448) is a storage type of
+ * paged caches alone (dresd_kv_cache). */
+typedef enum { DRESD_F32 = 0, DRESD_F16 = 1, DRESD_BF16 = 2, DRESD_F8 = 3 } dresd_dtype;
 
 typedef enum {
   DRESD_OK = 0,
@@ -317,6 +319,187 @@ dresd_status dresd_transform(const float *x, int64_t M, int32_t D, const float *
 dresd_status dresd_pack_drafts(const int32_t *tokens, int32_t B, int32_t k, int32_t L,
                                int32_t r, int32_t length, int32_t eos, int32_t *drafts,
                                int32_t *count, dresd_stream stream);
+
+/*
+ * Batch verification (Section 3.6).  The drafts of a step go through the
+ * language model in one forward beside the cached context, and the path that
+ * the model's own tokens follow is accepted.  The five calls below are what
+ * that forward needs around the model's weights:
+ *
+ *   dresd_draft_tree       drafts -> prefix tree: its tokens, parents, depths
+ *                          and, for the attention, every node's ancestors
+ *   dresd_kv_write         the tree's keys and values into the paged cache
+ *   dresd_paged_attention  its queries over the context and their ancestors
+ *   dresd_accept_drafts    the logits of its nodes -> the accepted path
+ *   dresd_kv_read          (with dresd_kv_write) the accepted path's entries
+ *                          out of the cache and into their final slots
+ *
+ * The same cache serves prompts, in chunks, and single tokens.  None of them
+ * allocates, synchronises or keeps state between calls; all can be captured.
+ */
+
+/* Most nodes of a draft tree. */
+#define DRESD_NODES_MAX 1024
+
+/*
+ * Prefix tree of each query's drafts.  Node 0 is next_tok[b]; draft by draft
+ * in rank order, each prefix that no earlier draft has becomes a node, so a
+ * parent's index is lower than its children's.  Drafts that do not start with
+ * next_tok[b] cannot be accepted and are left out, and a draft ends before its
+ * first EOS.  Nodes past the budget N are dropped.
+ *
+ *   drafts    device, [B, r, length] int32 (from dresd_pack_drafts).
+ *   count     device, [B] int32: drafts per query (rows past them are not read
+ *             as drafts; values outside [0, r] count as the nearer bound).
+ *   next_tok  device, [B] int32.
+ *   B >= 0 (0 is a no-op); 1 <= r <= DRESD_K_MAX; 1 <= length <= 4096;
+ *   1 <= N <= DRESD_NODES_MAX.  1 + r (length - 1) nodes always suffice.
+ *   token     device, [B, N] int32 out: token of each node, eos past the last.
+ *   parent    device, [B, N] int32 out: its parent, -1 for node 0 and past the
+ *             last node.
+ *   depth     device, [B, N] int32 out: its tokens after node 0 (so that the
+ *             node's position is node 0's plus its depth), 0 past the last.
+ *   mask      device, [B, N, W] uint64 out, W = (N + 63) / 64: bit v of row u
+ *             (bit v % 64 of word v / 64) is set where v is u or an ancestor of
+ *             u; 0 past the last node.  As dresd_paged_attention takes it.
+ *   nodes     device, [B] int32 out: nodes of each tree, >= 1.
+ * Deterministic.  Errors: EINVAL (null pointer with B > 0, sizes out of
+ * range), EDEVICE.
+ */
+dresd_status dresd_draft_tree(const int32_t *drafts, const int32_t *count,
+                              const int32_t *next_tok, int32_t B, int32_t r, int32_t length,
+                              int32_t eos, int32_t N, int32_t *token, int32_t *parent,
+                              int32_t *depth, uint64_t *mask, int32_t *nodes,
+                              dresd_stream stream);
+
+/*
+ * A paged cache of keys and values, in the caller's memory.  Slot s is row
+ * s % page_size of page s / page_size, for every head.
+ *   k, v          device, [pages, heads, page_size, dim], 16-byte aligned, element
+ *                 type dtype: DRESD_F16, DRESD_BF16 or DRESD_F8.
+ *   k_exp, v_exp  DRESD_F8: device, [pages, heads, page_size] uint8: a row's
+ *                 values are its stored ones times 2^(exp - 127).  NULL otherwise.
+ *   1 <= pages < 2^31; page_size a power of two, at most 65536;
+ *   1 <= heads <= 65535; dim a multiple of 8 in [8, 256].
+ */
+typedef struct {
+  void *k, *v;
+  uint8_t *k_exp, *v_exp;
+  int64_t pages;
+  int32_t page_size, heads, dim, dtype;
+} dresd_kv_cache;
+
+/*
+ * Write n tokens' keys and values into cache slots.
+ *   k, v      device, element type dtype (DRESD_F32, DRESD_F16 or DRESD_BF16):
+ *             element j of head h of token i is at i * row + h * head + j, in elements, with
+ *             strides of its own for k and v (slices of a projection's output
+ *             need no copy).  Pointers and strides are multiples of 16 bytes.
+ *   slots     device, [n] int64: each token's slot.  A token whose slot is outside
+ *             [0, pages * page_size) (-1, say) is skipped.  Two tokens of one call
+ *             must not share a slot (not checked: its contents would be a mixture).
+ *   n >= 0 (0 is a no-op).
+ * 16-bit caches hold the values rounded to nearest even.  DRESD_F8: a row (one
+ * token of one head) is stored at the smallest power of two, not below 2^-126,
+ * at which its largest magnitude is at most 448 (a zero row: 2^-9), its
+ * elements rounded to nearest even (but down where 2^128 would result);
+ * infinite elements are stored as NaN, as NaNs are, and do not take part in
+ * the largest magnitude.  A power of two scales without rounding, so rows read
+ * back in bf16 or fp32 are exactly the stored ones, and writing them again
+ * stores the same values.
+ * Errors: EINVAL (null pointer with n > 0, ranges, alignment, a dtype that does
+ * not fit), EDEVICE.
+ */
+dresd_status dresd_kv_write(const dresd_kv_cache *cache, const void *k, int64_t k_row,
+                            int64_t k_head, const void *v, int64_t v_row, int64_t v_head,
+                            int32_t dtype, const int64_t *slots, int64_t n,
+                            dresd_stream stream);
+
+/*
+ * Read cache slots back: k, v device, [n, heads, dim] out in dtype (DRESD_F32,
+ * DRESD_F16 or DRESD_BF16; rounded to nearest even), 16-byte aligned; slots device, [n]
+ * int64, in any order, repeats allowed.  A slot outside the cache gives zeros.
+ * Errors: as dresd_kv_write.
+ */
+dresd_status dresd_kv_read(const dresd_kv_cache *cache, const int64_t *slots, int64_t n,
+                           int32_t dtype, void *k, void *v, dresd_stream stream);
+
+/*
+ * Attention of a chunk of new tokens over a paged cache that holds their own
+ * keys and values already.  Sequence b has lengths[b] tokens in the cache, the last
+ * n_b of which are its chunk, and page table[b][p / page_size] holds its
+ * position p.  Row t of its chunk (position lengths[b] - n_b + t) sees the
+ * positions up to its own, or, with a mask, all positions before the chunk and
+ * those chunk tokens j whose bit j is set in its row of the mask:
+ *
+ *   out = sum_p e^(s_p - lse) v_p,   s_p = scale q . k_p,   lse = log sum_p e^(s_p)
+ *
+ * over the visible p.  A row that sees nothing gets zeros and lse -inf.
+ *
+ *   q         device, dtype DRESD_F16 or DRESD_BF16 (that of a 16-bit cache): head
+ *             h of row t is at t * q_row + h * q_head, in elements; pointer and
+ *             strides are multiples of 16 bytes.  Rows of all chunks follow one another.
+ *   q_heads   a multiple of the cache's heads: query head h reads cache head
+ *             h / (q_heads / heads).
+ *   starts    device, [B + 1] int32: sequence b's chunk is rows starts[b] to
+ *             starts[b + 1] - 1, n_b of them, possibly none; rows before
+ *             starts[0], from starts[B] on and outside [0, T) are left as they
+ *             were.  Or NULL: T = B n, and every chunk has n rows.
+ *   n         tokens per chunk without starts (ignored with them).
+ *   T         rows of q and out, T * q_heads < 2^31; T = 0 is a no-op.
+ *   table     device, [B, width] int32, width >= 1: page ids.  Positions past the
+ *             table and pages outside [0, pages) hold nothing: they are not seen.
+ *   lengths   device, [B] int32.
+ *   mask      device, [T, words] uint64 (bits past the words are unset), or NULL.
+ *   scale     finite.
+ *   out       device, [T, q_heads, dim] in dtype, 16-byte aligned.
+ *   lse       device, [T, q_heads] fp32 (natural logarithm), or NULL.
+ *   work      device, work_bytes of workspace, 16-byte aligned: at least what
+ *             dresd_paged_attention_workspace says for these arguments (which
+ *             reads no device memory).  Used by this call alone until `stream`
+ *             has completed it; its contents do not matter.
+ * What masked positions hold does not matter, infinities and NaN included.
+ * Scores, softmax statistics and sums are fp32; keys and queries enter the
+ * matrix cores unrounded, a row's weights rounded to dtype.  Deterministic.
+ * Errors: EINVAL (null pointer with T > 0, ranges, alignment, dtypes that do not
+ * fit, too little workspace), EDEVICE.
+ */
+dresd_status dresd_paged_attention(const dresd_kv_cache *cache, const void *q, int64_t q_row,
+                                   int64_t q_head, int32_t dtype, int32_t q_heads,
+                                   const int32_t *starts, int32_t n, int32_t B, int64_t T,
+                                   const int32_t *table, int32_t width, const int32_t *lengths,
+                                   const uint64_t *mask, int32_t words, float scale, void *out,
+                                   float *lse, void *work, int64_t work_bytes,
+                                   dresd_stream stream);
+dresd_status dresd_paged_attention_workspace(const dresd_kv_cache *cache, int32_t q_heads,
+                                             int32_t ragged, int32_t n, int32_t B, int64_t T,
+                                             int32_t width, int64_t *bytes);
+
+/*
+ * Acceptance of a draft tree by the model's own greedy tokens: from node 0,
+ * with g the token of the largest logit of the present node (ties to the lower
+ * token; NaN is below everything, and a row of nothing else gives token 0), go on
+ * to the lowest-numbered child whose token is g, while there is one and fewer
+ * than `most` nodes are accepted.
+ *
+ *   logits    device, dtype (DRESD_F32, DRESD_F16 or DRESD_BF16): row u of query
+ *             b starts at (b N + u) * row elements, row >= V.
+ *   token, parent  device, [B, N] int32, nodes device, [B] int32: the tree
+ *             (dresd_draft_tree; nodes outside [0, N] count as the nearer bound).
+ *   B >= 0 (0 is a no-op); 1 <= N <= DRESD_NODES_MAX; 1 <= V < 2^31;
+ *   1 <= most <= DRESD_NODES_MAX.
+ *   path      device, [B, most] int32 out: the accepted nodes, -1 past them.
+ *   accepted  device, [B] int32 out: their number, >= 1 (0 for an empty tree).
+ *   next_tok  device, [B] int32 out: the model's token after the last of them (-1
+ *             for an empty tree).
+ * Deterministic.  Errors: EINVAL (null pointer with B > 0, sizes out of range),
+ * EDEVICE.
+ */
+dresd_status dresd_accept_drafts(const void *logits, int32_t dtype, int64_t row, int32_t V,
+                                 const int32_t *token, const int32_t *parent,
+                                 const int32_t *nodes, int32_t B, int32_t N, int32_t most,
+                                 int32_t *path, int32_t *accepted, int32_t *next_tok,
+                                 dresd_stream stream);
 
 /*
  * Describe how the next search of this shape would run (host outputs, NULL

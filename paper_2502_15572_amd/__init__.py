@@ -12,9 +12,10 @@ from __future__ import annotations
 import ctypes
 
 from . import _lib
-from ._lib import DresdError, K_MAX  # noqa: F401
+from ._lib import DresdError, K_MAX, NODES_MAX  # noqa: F401
 
 __all__ = ["Index", "PartitionedIndex", "DresdError", "K_MAX", "transform", "pack_drafts",
+           "draft_tree", "kv_write", "kv_read", "paged_attention", "accept_drafts", "NODES_MAX",
            "kmeans_assign", "kmeans_update", "kmeans_init", "train_partitions", "bw_probe",
            "release_cached"]
 
@@ -357,6 +358,278 @@ def pack_drafts(tokens, r: int, length: int, eos: int = 0, out=None, stream=None
                                      int(eos), ctypes.c_void_p(drafts.data_ptr()),
                                      ctypes.c_void_p(count.data_ptr()), _stream_handle(stream)))
     return drafts, count
+
+
+# ---- batch verification: the forward over the drafts, around the model's weights -----------
+
+
+def _on(stream, *tensors):
+    """Context in which a call on these GPU tensors allocates and launches: their device, and
+    ``stream`` (outputs and workspaces then belong to it, and a later call on it may reuse
+    them)."""
+    import contextlib
+
+    import torch
+    device = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise TypeError("all inputs must be GPU tensors")
+        if device is None:
+            device = t.device
+        elif t.device != device:
+            raise ValueError("all tensors must be on one device")
+    if stream is not None:
+        if stream.device != device:
+            raise ValueError("the stream must be on the tensors' device")
+        return torch.cuda.stream(stream)
+    if device.index != torch.cuda.current_device():
+        return torch.cuda.device(device)
+    return contextlib.nullcontext()
+
+
+def _expect(name, t, dtype, *shape):
+    """A contiguous tensor of this type and shape (None: any size)."""
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
+    if t.dim() != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape)):
+        raise ValueError("%s must have shape %s, not %s"
+                         % (name, list("?" if w is None else w for w in shape), list(t.shape)))
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _stride(t, d):
+    """Stride of a dimension (0 where it is never taken)."""
+    return t.stride(d) if t.shape[d] > 1 else 0
+
+
+def draft_tree(drafts, count, next_tok, nodes: int | None = None, eos: int = 0, out=None,
+               stream=None):
+    """Prefix tree of each query's drafts (Section 3.6), the tokens that one
+    forward verifies: ``drafts`` [B, r, length] and ``count`` [B] int32 from
+    ``pack_drafts``, ``next_tok`` [B] int32, the token they start with, which is
+    node 0.  Draft by draft in rank order every new prefix is a node, up to
+    ``nodes`` of them (default: as many as the shape can need, at most
+    ``NODES_MAX``).  Returns (token [B, N], parent [B, N], depth [B, N] int32, mask
+    [B, N, ceil(N / 64)] int64, nodes [B] int32): bit v of a node's mask row is
+    set where v is the node or its ancestor (as ``paged_attention`` takes it),
+    depth counts its tokens after node 0; past a query's last node the token is
+    ``eos``, the parent -1, depth and mask 0."""
+    import torch
+    i32 = torch.int32
+    _expect("drafts", drafts, i32, None, None, None)
+    B, r, length = drafts.shape
+    _expect("count", count, i32, B)
+    _expect("next_tok", next_tok, i32, B)
+    N = min(NODES_MAX, 1 + r * max(0, length - 1)) if nodes is None else int(nodes)
+    if not 1 <= N <= NODES_MAX:
+        raise ValueError("nodes must be in [1, %d]" % NODES_MAX)
+    W = (N + 63) // 64
+    with _on(stream, drafts, count, next_tok, *(out or ())):
+        if out is None:
+            dev = drafts.device
+            out = (torch.empty((B, N), dtype=i32, device=dev),
+                   torch.empty((B, N), dtype=i32, device=dev),
+                   torch.empty((B, N), dtype=i32, device=dev),
+                   torch.empty((B, N, W), dtype=torch.int64, device=dev),
+                   torch.empty((B,), dtype=i32, device=dev))
+        else:
+            for name, t in zip(("token", "parent", "depth"), out):
+                _expect(name, t, i32, B, N)
+            _expect("mask", out[3], torch.int64, B, N, W)
+            _expect("nodes", out[4], i32, B)
+        _lib.check(_lib.load().dresd_draft_tree(
+            drafts.data_ptr(), count.data_ptr(), next_tok.data_ptr(), B, r, length, int(eos), N,
+            *(t.data_ptr() for t in out), _stream_handle()))
+    return tuple(out)
+
+
+_CACHE_DTYPES = None
+
+
+def _kv_cache(k_pages, v_pages, k_exp, v_exp):
+    """The C description of a paged cache."""
+    import torch
+    global _CACHE_DTYPES
+    if _CACHE_DTYPES is None:
+        _CACHE_DTYPES = {torch.float16: _lib.F16, torch.bfloat16: _lib.BF16,
+                         torch.float8_e4m3fn: _lib.F8}
+    code = _CACHE_DTYPES.get(k_pages.dtype)
+    if code is None:
+        raise TypeError("a cache is float16, bfloat16 or float8_e4m3fn, not %s" % k_pages.dtype)
+    _expect("k_pages", k_pages, k_pages.dtype, None, None, None, None)
+    _expect("v_pages", v_pages, k_pages.dtype, *k_pages.shape)
+    P, H, page, D = k_pages.shape
+    if (code == _lib.F8) != (k_exp is not None) or (k_exp is None) != (v_exp is None):
+        raise ValueError("an 8-bit cache has k_exp and v_exp, a 16-bit one neither")
+    if k_exp is not None:
+        _expect("k_exp", k_exp, torch.uint8, P, H, page)
+        _expect("v_exp", v_exp, torch.uint8, P, H, page)
+    return _lib.KvCache(k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_exp), _ptr(v_exp), P, page,
+                        H, D, code)
+
+
+def kv_write(k, v, slots, k_pages, v_pages, k_exp=None, v_exp=None, stream=None) -> None:
+    """Write tokens' keys and values ([n, heads, dim], float32, float16 or
+    bfloat16; slices of a projection's output need no copy) into the slots
+    (int64 [n]) of a paged cache: ``k_pages`` and ``v_pages`` [pages, heads,
+    page_size, dim], slot s being row s % page_size of page s // page_size.  The
+    cache is float16, bfloat16, or float8_e4m3fn with a power of two a row (one token
+    of one head) in ``k_exp`` and ``v_exp`` (uint8 [pages, heads, page_size]): the
+    row's values are the stored ones times 2 ** (exp - 127).  Tokens whose slot
+    is outside the cache (-1, say) are skipped; two tokens must not share a slot."""
+    import torch
+    if k.dim() != 3 or k.shape != v.shape or k.dtype != v.dtype:
+        raise ValueError("k and v must be [n, heads, dim] of one type")
+    n = int(k.shape[0])
+    cache = _kv_cache(k_pages, v_pages, k_exp, v_exp)
+    if k.shape[1] != cache.heads or k.shape[2] != cache.dim:
+        raise ValueError("k and v must be [n, %d, %d]" % (cache.heads, cache.dim))
+    if k.stride(2) != 1 or v.stride(2) != 1:
+        raise ValueError("the last dimension of k and v must be contiguous")
+    _expect("slots", slots, torch.int64, n)
+    with _on(stream, k, v, slots, k_pages, v_pages, k_exp, v_exp):
+        _lib.check(_lib.load().dresd_kv_write(
+            cache, k.data_ptr(), _stride(k, 0), _stride(k, 1), v.data_ptr(), _stride(v, 0),
+            _stride(v, 1), _dtype_code(k), slots.data_ptr(), n, _stream_handle()))
+
+
+def kv_read(slots, k_pages, v_pages, k_exp=None, v_exp=None, dtype=None, out=None, stream=None):
+    """Keys and values of cache slots (int64 [n], any order, repeats allowed;
+    zeros for a slot outside the cache) as (k, v) [n, heads, dim] in ``dtype``
+    (float32, float16 or bfloat16; default: the cache's, bfloat16 for 8-bit caches,
+    which holds their values exactly)."""
+    import torch
+    cache = _kv_cache(k_pages, v_pages, k_exp, v_exp)
+    _expect("slots", slots, torch.int64, None)
+    n = int(slots.shape[0])
+    if dtype is None:
+        dtype = torch.bfloat16 if cache.dtype == _lib.F8 else k_pages.dtype
+    with _on(stream, slots, k_pages, v_pages, k_exp, v_exp, *(out or ())):
+        if out is None:
+            shape = (n, cache.heads, cache.dim)
+            out = (torch.empty(shape, dtype=dtype, device=slots.device),
+                   torch.empty(shape, dtype=dtype, device=slots.device))
+        else:
+            _expect("k", out[0], dtype, n, cache.heads, cache.dim)
+            _expect("v", out[1], dtype, n, cache.heads, cache.dim)
+        _lib.check(_lib.load().dresd_kv_read(
+            cache, slots.data_ptr(), n, _dtype_code(out[0]), out[0].data_ptr(),
+            out[1].data_ptr(), _stream_handle()))
+    return tuple(out)
+
+
+def paged_attention(q, k_pages, v_pages, table, lengths, starts=None, mask=None, k_exp=None,
+                    v_exp=None, scale: float | None = None, with_lse: bool = False, out=None,
+                    stream=None):
+    """Attention of each sequence's newest tokens, its chunk (one decoded token, a
+    draft tree, a piece of a prompt), over a paged cache that holds them already
+    (``kv_write``).  Sequence b has ``lengths[b]`` (int32 [B]) tokens in the cache,
+    the last of them its chunk, and its position p in page ``table[b, p // page_size]``
+    (int32 [B, width]).  ``q`` (float16 or bfloat16, that of a 16-bit cache) is
+    [B, n, q_heads, dim], or [T, q_heads, dim] with sequence b's chunk in rows
+    ``starts[b]`` to ``starts[b + 1] - 1`` (int32 [B + 1]); query head h reads
+    cache head h // (q_heads // heads).  A row sees the positions up to its own;
+    with ``mask`` (int64 [B, n, words] or [T, words]; ``draft_tree``) all before the
+    chunk and the chunk tokens whose bit is set.  ``scale`` defaults to dim ** -0.5.
+    Returns the output, shaped as q and in its type (zeros for a row that sees
+    nothing; rows outside every chunk are left as they were), and with ``with_lse``
+    also the fp32 logarithms of the rows' sums ([..., q_heads]; -inf for a row
+    that sees nothing).  ``out``: the output tensor, or the pair."""
+    import torch
+    cache = _kv_cache(k_pages, v_pages, k_exp, v_exp)
+    B = int(lengths.shape[0]) if lengths.dim() == 1 else -1
+    _expect("lengths", lengths, torch.int32, None)
+    _expect("table", table, torch.int32, B, None)
+    if q.dtype not in (torch.float16, torch.bfloat16):
+        raise TypeError("q must be float16 or bfloat16, not %s" % q.dtype)
+    if starts is None:
+        if q.dim() != 4 or q.shape[0] != B:
+            raise ValueError("without starts q must be [%d, n, q_heads, dim]" % B)
+        n = int(q.shape[1])
+        T, row = B * n, _stride(q, 1 if n > 1 else 0)
+        if n > 1 and B > 1 and q.stride(0) != n * q.stride(1):
+            raise ValueError("q's tokens must be evenly spaced")
+    else:
+        _expect("starts", starts, torch.int32, B + 1)
+        if q.dim() != 3:
+            raise ValueError("with starts q must be [T, q_heads, dim]")
+        n, T, row = 0, int(q.shape[0]), _stride(q, 0)
+    H = int(q.shape[-2])
+    if q.shape[-1] != cache.dim or q.stride(-1) != 1:
+        raise ValueError("q's last dimension must be %d contiguous elements" % cache.dim)
+    words = 0
+    if mask is not None:
+        _expect("mask", mask, torch.int64, *q.shape[:-2], None)
+        words = int(mask.shape[-1])
+    if scale is None:
+        scale = cache.dim ** -0.5
+    given = out if isinstance(out, (tuple, list)) else () if out is None else (out,)
+    lib = _lib.load()
+    with _on(stream, q, k_pages, v_pages, k_exp, v_exp, table, lengths, starts, mask, *given):
+        if not given:
+            o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device) \
+                if with_lse else None
+        else:
+            o, lse = given[0], given[1] if len(given) > 1 else None
+            if (lse is not None) != with_lse:
+                raise ValueError("out must be the pair exactly with with_lse")
+            _expect("out", o, q.dtype, *q.shape)
+            if lse is not None:
+                _expect("lse", lse, torch.float32, *q.shape[:-1])
+        need = ctypes.c_int64()
+        _lib.check(lib.dresd_paged_attention_workspace(
+            cache, H, starts is not None, n, B, T, int(table.shape[1]), ctypes.byref(need)))
+        work = torch.empty(need.value, dtype=torch.uint8, device=q.device) if need.value else None
+        _lib.check(lib.dresd_paged_attention(
+            cache, q.data_ptr(), row, _stride(q, -2), _dtype_code(q), H, _ptr(starts), n, B, T,
+            table.data_ptr(), int(table.shape[1]), lengths.data_ptr(), _ptr(mask), words,
+            float(scale), o.data_ptr(), _ptr(lse), _ptr(work), need.value, _stream_handle()))
+    return (o, lse) if with_lse else o
+
+
+def accept_drafts(logits, token, parent, nodes, most: int | None = None, out=None, stream=None):
+    """Acceptance of a draft tree (``draft_tree``'s token, parent [B, N] and nodes
+    [B]) by the model's own greedy tokens: from node 0, on to the child that holds
+    the token of the node's largest logit (ties to the lower token), while there
+    is one and fewer than ``most`` (default N) nodes are accepted.  ``logits``
+    [B, N, V] float32, float16 or bfloat16, rows evenly spaced.  Returns (path [B,
+    most] int32: the accepted nodes, then -1; accepted [B] int32: their number;
+    next_tok [B] int32: the model's token after the last of them)."""
+    import torch
+    i32 = torch.int32
+    if logits.dim() != 3:
+        raise ValueError("logits must be [B, N, V]")
+    B, N, V = logits.shape
+    row = _stride(logits, 1 if N > 1 else 0)
+    if logits.stride(2) != 1 and V > 1 or (N > 1 and B > 1 and logits.stride(0) != N * row):
+        raise ValueError("the rows of logits must be contiguous and evenly spaced")
+    _expect("token", token, i32, B, N)
+    _expect("parent", parent, i32, B, N)
+    _expect("nodes", nodes, i32, B)
+    most = N if most is None else int(most)
+    with _on(stream, logits, token, parent, nodes, *(out or ())):
+        if out is None:
+            dev = logits.device
+            out = (torch.empty((B, most), dtype=i32, device=dev),
+                   torch.empty((B,), dtype=i32, device=dev),
+                   torch.empty((B,), dtype=i32, device=dev))
+        else:
+            _expect("path", out[0], i32, B, most)
+            _expect("accepted", out[1], i32, B)
+            _expect("next_tok", out[2], i32, B)
+        _lib.check(_lib.load().dresd_accept_drafts(
+            logits.data_ptr(), _dtype_code(logits), max(row, V), V, token.data_ptr(),
+            parent.data_ptr(), nodes.data_ptr(), B, N, most, *(t.data_ptr() for t in out),
+            _stream_handle()))
+    return tuple(out)
 
 
 def _rows(x):

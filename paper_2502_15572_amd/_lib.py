@@ -15,7 +15,8 @@ LIB_PATH = os.path.join(HERE, "libdresd.so")
 
 OK, EINVAL, ENOMEM, EDEVICE, EUNSUPPORTED = 0, 1, 2, 3, 4
 K_MAX = 1024
-F32, F16, BF16 = 0, 1, 2
+NODES_MAX = 1024
+F32, F16, BF16, F8 = 0, 1, 2, 3
 
 EXPORTS = ["dresd_index_create", "dresd_search", "dresd_index_info", "dresd_index_destroy",
            "dresd_last_error", "dresd_profile_enable", "dresd_profile_read",
@@ -25,7 +26,8 @@ EXPORTS = ["dresd_index_create", "dresd_search", "dresd_index_info", "dresd_inde
            "dresd_ivf_create_by_token", "dresd_ivf_search_next_token", "dresd_ivf_profile_enable",
            "dresd_ivf_profile_read", "dresd_kmeans_assign", "dresd_kmeans_update",
            "dresd_kmeans_init", "dresd_bw_probe", "dresd_search_noalloc",
-           "dresd_release_cached"]
+           "dresd_release_cached", "dresd_draft_tree", "dresd_kv_write", "dresd_kv_read",
+           "dresd_paged_attention", "dresd_paged_attention_workspace", "dresd_accept_drafts"]
 
 _lock = threading.Lock()
 _lib = None
@@ -35,6 +37,14 @@ class DresdError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__("dresd status %d: %s" % (status, msg))
         self.status = status
+
+
+class KvCache(ctypes.Structure):
+    """dresd_kv_cache"""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p),
+                ("v_exp", ctypes.c_void_p), ("pages", ctypes.c_int64),
+                ("page_size", ctypes.c_int32), ("heads", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
 
 
 def _declare(lib):
@@ -101,6 +111,21 @@ def _declare(lib):
     lib.dresd_bw_probe.restype = ctypes.c_int
     lib.dresd_search_noalloc.argtypes = [P, P, I32, I32, P, P, P, P]
     lib.dresd_search_noalloc.restype = ctypes.c_int
+    C = ctypes.POINTER(KvCache)
+    lib.dresd_draft_tree.argtypes = [P, P, P, I32, I32, I32, I32, I32, P, P, P, P, P, P]
+    lib.dresd_draft_tree.restype = ctypes.c_int
+    lib.dresd_kv_write.argtypes = [C, P, I64, I64, P, I64, I64, I32, P, I64, P]
+    lib.dresd_kv_write.restype = ctypes.c_int
+    lib.dresd_kv_read.argtypes = [C, P, I64, I32, P, P, P]
+    lib.dresd_kv_read.restype = ctypes.c_int
+    lib.dresd_paged_attention.argtypes = [C, P, I64, I64, I32, I32, P, I32, I32, I64, P, I32, P, P,
+                                          I32, F, P, P, P, I64, P]
+    lib.dresd_paged_attention.restype = ctypes.c_int
+    lib.dresd_paged_attention_workspace.argtypes = [C, I32, I32, I32, I32, I64, I32,
+                                                    ctypes.POINTER(I64)]
+    lib.dresd_paged_attention_workspace.restype = ctypes.c_int
+    lib.dresd_accept_drafts.argtypes = [P, I32, I64, I32, P, P, P, I32, I32, I32, P, P, P, P]
+    lib.dresd_accept_drafts.restype = ctypes.c_int
     return lib
 
 

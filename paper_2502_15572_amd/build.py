@@ -38,6 +38,8 @@ UNITS = [("dresd_kernels.hip", ["-DDRESD_TU=%d" % t], "kernels%d" % t) for t in 
     ("dresd_kmeans.hip", [], "kmeans"), ("dresd_assign.hip", [], "assign"),
     ("dresd_group.hip", [], "group"), ("dresd_layout.hip", [], "layout"),
     ("dresd_project.hip", [], "project"), ("dresd_bwprobe.hip", [], "bwprobe"),
+    ("dresd_tree.hip", [], "tree"), ("dresd_kv.hip", [], "kv"),
+    ("dresd_attend.hip", [], "attend"),
     ("dresd_runtime.hip", [], "runtime")]
 
 

@@ -15,6 +15,7 @@
 
 #include "dresd_internal.h"
 #include "dresd_ops.h"
+#include "dresd_verify.h"
 
 using namespace dresd;
 
@@ -1436,6 +1437,257 @@ dresd_status dresd_pack_drafts(const int32_t *tokens, int32_t B, int32_t k, int3
   p.length = length;
   p.eos = eos;
   DRESD_HIP(launch_pack_drafts(p, static_cast<hipStream_t>(stream)));
+  return DRESD_OK;
+}
+
+dresd_status dresd_draft_tree(const int32_t *drafts, const int32_t *count,
+                              const int32_t *next_tok, int32_t B, int32_t r, int32_t length,
+                              int32_t eos, int32_t N, int32_t *token, int32_t *parent,
+                              int32_t *depth, uint64_t *mask, int32_t *nodes,
+                              dresd_stream stream) {
+  if (B < 0) return fail(DRESD_EINVAL, "B must be >= 0");
+  if (r < 1 || r > DRESD_K_MAX) return fail(DRESD_EINVAL, "r must be in [1, DRESD_K_MAX]");
+  if (length < 1 || length > 4096) return fail(DRESD_EINVAL, "length out of range");
+  if (N < 1 || N > DRESD_NODES_MAX) return fail(DRESD_EINVAL, "N must be in [1, DRESD_NODES_MAX]");
+  if (B == 0) return DRESD_OK;
+  if (!drafts || !count || !next_tok || !token || !parent || !depth || !mask || !nodes)
+    return fail(DRESD_EINVAL, "NULL pointer argument");
+  TreeParams p;
+  p.drafts = drafts;
+  p.count = count;
+  p.next_tok = next_tok;
+  p.token = token;
+  p.parent = parent;
+  p.depth = depth;
+  p.mask = mask;
+  p.nodes = nodes;
+  p.B = B;
+  p.r = r;
+  p.length = length;
+  p.eos = eos;
+  p.N = N;
+  DRESD_HIP(launch_draft_tree(p, static_cast<hipStream_t>(stream)));
+  return DRESD_OK;
+}
+
+dresd_status dresd_accept_drafts(const void *logits, int32_t dtype, int64_t row, int32_t V,
+                                 const int32_t *token, const int32_t *parent,
+                                 const int32_t *nodes, int32_t B, int32_t N, int32_t most,
+                                 int32_t *path, int32_t *accepted, int32_t *next_tok,
+                                 dresd_stream stream) {
+  if (B < 0) return fail(DRESD_EINVAL, "B must be >= 0");
+  if (dtype < DRESD_F32 || dtype > DRESD_BF16) return fail(DRESD_EINVAL, "unknown dtype");
+  if (V < 1 || V > (1 << 30)) return fail(DRESD_EINVAL, "V out of range");
+  if (row < V || row > ((int64_t)1 << 40)) return fail(DRESD_EINVAL, "row out of range");
+  if (N < 1 || N > DRESD_NODES_MAX) return fail(DRESD_EINVAL, "N must be in [1, DRESD_NODES_MAX]");
+  if (most < 1 || most > DRESD_NODES_MAX)
+    return fail(DRESD_EINVAL, "most must be in [1, DRESD_NODES_MAX]");
+  if (B == 0) return DRESD_OK;
+  if (!logits || !token || !parent || !nodes || !path || !accepted || !next_tok)
+    return fail(DRESD_EINVAL, "NULL pointer argument");
+  if ((uintptr_t)logits % (dtype == DRESD_F32 ? 4 : 2))
+    return fail(DRESD_EINVAL, "logits must be aligned to their elements");
+  AcceptParams p;
+  p.logits = logits;
+  p.row = row;
+  p.token = token;
+  p.parent = parent;
+  p.nodes = nodes;
+  p.path = path;
+  p.accepted = accepted;
+  p.next_tok = next_tok;
+  p.B = B;
+  p.N = N;
+  p.V = V;
+  p.most = most;
+  p.dtype = dtype;
+  DRESD_HIP(launch_accept(p, static_cast<hipStream_t>(stream)));
+  return DRESD_OK;
+}
+
+namespace {
+
+// The cache's description, checked but for its pointers.
+dresd_status check_cache(const dresd_kv_cache *c, CacheRef *out) {
+  if (!c) return fail(DRESD_EINVAL, "cache is NULL");
+  if (c->dtype < DRESD_F16 || c->dtype > DRESD_F8) return fail(DRESD_EINVAL, "unknown cache dtype");
+  if (c->pages < 1 || c->pages > 0x7fffffffLL) return fail(DRESD_EINVAL, "pages out of range");
+  if (c->page_size < 1 || c->page_size > 65536 || (c->page_size & (c->page_size - 1)))
+    return fail(DRESD_EINVAL, "page_size must be a power of two, at most 65536");
+  if (c->heads < 1 || c->heads > 65535) return fail(DRESD_EINVAL, "heads out of range");
+  if (c->dim < 8 || c->dim > kHeadDimMax || c->dim % 8)
+    return fail(DRESD_EINVAL, "dim must be a multiple of 8 in [8, 256]");
+  out->k = c->k;
+  out->v = c->v;
+  out->k_exp = c->k_exp;
+  out->v_exp = c->v_exp;
+  out->pages = c->pages;
+  out->page_log = __builtin_ctz((unsigned)c->page_size);
+  out->heads = c->heads;
+  out->dim = c->dim;
+  out->dtype = c->dtype;
+  return DRESD_OK;
+}
+
+dresd_status check_cache_memory(const CacheRef &c) {
+  if (!c.k || !c.v) return fail(DRESD_EINVAL, "NULL pointer argument");
+  if (((uintptr_t)c.k | (uintptr_t)c.v) % 16)
+    return fail(DRESD_EINVAL, "cache pages must be 16-byte aligned");
+  if (c.dtype == kF8 && (!c.k_exp || !c.v_exp))
+    return fail(DRESD_EINVAL, "an 8-bit cache needs its exponents");
+  return DRESD_OK;
+}
+
+// Pointer and element strides that 16-byte loads can follow.
+bool rows_aligned(const void *p, int64_t row, int64_t head, int elem) {
+  return (uintptr_t)p % 16 == 0 && row * elem % 16 == 0 && head * elem % 16 == 0;
+}
+
+constexpr int64_t kStrideMax = (int64_t)1 << 40;
+bool stride_ok(int64_t s) { return s >= 0 && s <= kStrideMax; }
+
+dresd_status check_tokens(const CacheRef &c, int64_t n, int32_t dtype) {
+  if (dtype < DRESD_F32 || dtype > DRESD_BF16) return fail(DRESD_EINVAL, "unknown dtype");
+  if (n < 0 || n > 0x7fffffffLL / c.heads) return fail(DRESD_EINVAL, "n out of range");
+  return DRESD_OK;
+}
+
+}  // namespace
+
+dresd_status dresd_kv_write(const dresd_kv_cache *cache, const void *k, int64_t k_row,
+                            int64_t k_head, const void *v, int64_t v_row, int64_t v_head,
+                            int32_t dtype, const int64_t *slots, int64_t n,
+                            dresd_stream stream) {
+  KvParams p = {};
+  dresd_status s = check_cache(cache, &p.c);
+  if (s == DRESD_OK) s = check_tokens(p.c, n, dtype);
+  if (s != DRESD_OK) return s;
+  if (!stride_ok(k_row) || !stride_ok(k_head) || !stride_ok(v_row) || !stride_ok(v_head))
+    return fail(DRESD_EINVAL, "stride out of range");
+  if (n == 0) return DRESD_OK;
+  if ((s = check_cache_memory(p.c)) != DRESD_OK) return s;
+  if (!k || !v || !slots) return fail(DRESD_EINVAL, "NULL pointer argument");
+  const int elem = dtype == DRESD_F32 ? 4 : 2;
+  if (!rows_aligned(k, k_row, k_head, elem) || !rows_aligned(v, v_row, v_head, elem))
+    return fail(DRESD_EINVAL, "rows of keys and values must be 16-byte aligned");
+  p.k_in = k;
+  p.k_row = k_row;
+  p.k_head = k_head;
+  p.v_in = v;
+  p.v_row = v_row;
+  p.v_head = v_head;
+  p.slots = slots;
+  p.n = n;
+  p.dtype = dtype;
+  DRESD_HIP(launch_kv_write(p, static_cast<hipStream_t>(stream)));
+  return DRESD_OK;
+}
+
+dresd_status dresd_kv_read(const dresd_kv_cache *cache, const int64_t *slots, int64_t n,
+                           int32_t dtype, void *k, void *v, dresd_stream stream) {
+  KvParams p = {};
+  dresd_status s = check_cache(cache, &p.c);
+  if (s == DRESD_OK) s = check_tokens(p.c, n, dtype);
+  if (s != DRESD_OK) return s;
+  if (n == 0) return DRESD_OK;
+  if ((s = check_cache_memory(p.c)) != DRESD_OK) return s;
+  if (!k || !v || !slots) return fail(DRESD_EINVAL, "NULL pointer argument");
+  if (((uintptr_t)k | (uintptr_t)v) % 16)
+    return fail(DRESD_EINVAL, "outputs must be 16-byte aligned");
+  p.k_out = k;
+  p.v_out = v;
+  p.slots = slots;
+  p.n = n;
+  p.dtype = dtype;
+  DRESD_HIP(launch_kv_read(p, static_cast<hipStream_t>(stream)));
+  return DRESD_OK;
+}
+
+namespace {
+
+// What the launch plan of an attention goes by.
+dresd_status attend_shape(const dresd_kv_cache *cache, int32_t q_heads, bool ragged, int32_t n,
+                          int32_t B, int64_t T, int32_t width, AttendParams *p) {
+  dresd_status s = check_cache(cache, &p->c);
+  if (s != DRESD_OK) return s;
+  if (q_heads < 1 || q_heads % p->c.heads)
+    return fail(DRESD_EINVAL, "q_heads must be a multiple of the cache's heads");
+  if (B < 0) return fail(DRESD_EINVAL, "B must be >= 0");
+  if (T < 0 || T > 0x7fffffffLL / q_heads) return fail(DRESD_EINVAL, "T out of range");
+  if (!ragged && (n < 0 || (int64_t)n * B != T)) return fail(DRESD_EINVAL, "T must be B n");
+  if (width < 1) return fail(DRESD_EINVAL, "width must be >= 1");
+  p->q_heads = q_heads;
+  p->n = n;
+  p->B = B;
+  p->T = T;
+  p->ragged = ragged;
+  p->width = width;
+  return DRESD_OK;
+}
+
+dresd_status compute_units(int *cus) {
+  int dev = 0;
+  DRESD_HIP(hipGetDevice(&dev));
+  DRESD_HIP(hipDeviceGetAttribute(cus, hipDeviceAttributeMultiprocessorCount, dev));
+  return DRESD_OK;
+}
+
+}  // namespace
+
+dresd_status dresd_paged_attention_workspace(const dresd_kv_cache *cache, int32_t q_heads,
+                                             int32_t ragged, int32_t n, int32_t B, int64_t T,
+                                             int32_t width, int64_t *bytes) {
+  if (!bytes) return fail(DRESD_EINVAL, "NULL pointer argument");
+  AttendParams p = {};
+  int cus = 0;
+  dresd_status s = attend_shape(cache, q_heads, ragged != 0, n, B, T, width, &p);
+  if (s == DRESD_OK) s = compute_units(&cus);
+  if (s != DRESD_OK) return s;
+  *bytes = attend_workspace(p, cus);
+  return DRESD_OK;
+}
+
+dresd_status dresd_paged_attention(const dresd_kv_cache *cache, const void *q, int64_t q_row,
+                                   int64_t q_head, int32_t dtype, int32_t q_heads,
+                                   const int32_t *starts, int32_t n, int32_t B, int64_t T,
+                                   const int32_t *table, int32_t width, const int32_t *lengths,
+                                   const uint64_t *mask, int32_t words, float scale, void *out,
+                                   float *lse, void *work, int64_t work_bytes,
+                                   dresd_stream stream) {
+  AttendParams p = {};
+  int cus = 0;
+  dresd_status s = attend_shape(cache, q_heads, starts != nullptr, n, B, T, width, &p);
+  if (s != DRESD_OK) return s;
+  if (dtype != DRESD_F16 && dtype != DRESD_BF16)
+    return fail(DRESD_EINVAL, "queries must be f16 or bf16");
+  if (p.c.dtype != kF8 && p.c.dtype != dtype)
+    return fail(DRESD_EINVAL, "queries must have the type of a 16-bit cache");
+  if (!stride_ok(q_row) || !stride_ok(q_head)) return fail(DRESD_EINVAL, "stride out of range");
+  if (mask && (words < 1 || words > 65536)) return fail(DRESD_EINVAL, "words out of range");
+  if (!(fabsf(scale) < HUGE_VALF)) return fail(DRESD_EINVAL, "scale must be finite");
+  if (T == 0 || B == 0) return DRESD_OK;
+  if ((s = check_cache_memory(p.c)) != DRESD_OK) return s;
+  if (!q || !table || !lengths || !out) return fail(DRESD_EINVAL, "NULL pointer argument");
+  if (!rows_aligned(q, q_row, q_head, 2) || (uintptr_t)out % 16)
+    return fail(DRESD_EINVAL, "rows of queries and output must be 16-byte aligned");
+  p.q = q;
+  p.q_row = q_row;
+  p.q_head = q_head;
+  p.starts = starts;
+  p.table = table;
+  p.lengths = lengths;
+  p.mask = mask;
+  p.words = words;
+  p.scale = scale;
+  p.out = out;
+  p.lse = lse;
+  p.work = work;
+  p.dtype = dtype;
+  if ((s = compute_units(&cus)) != DRESD_OK) return s;
+  const int64_t need = attend_workspace(p, cus);
+  if (need > 0 && (!work || work_bytes < need || (uintptr_t)work % 16))
+    return fail(DRESD_EINVAL, "workspace of " + std::to_string(need) + " bytes needed");
+  DRESD_HIP(launch_attend(p, cus, static_cast<hipStream_t>(stream)));
   return DRESD_OK;
 }
 
