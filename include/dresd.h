@@ -447,9 +447,10 @@ dresd_status dresd_kv_read(const dresd_kv_cache *cache, const int64_t *slots, in
  *             were.  Or NULL: T = B n, and every chunk has n rows.
  *   n         tokens per chunk without starts (ignored with them).
  *   T         rows of q and out, T * q_heads < 2^31; T = 0 is a no-op.
- *   table     device, [B, width] int32, width >= 1: page ids.  Positions past the
- *             table and pages outside [0, pages) hold nothing: they are not seen.
- *   lengths   device, [B] int32.
+ *   table     device, [B, width] int32, width >= 1, 0 <= B heads <= 2^30: page ids.
+ *             Positions past the table and pages outside [0, pages) hold nothing:
+ *             they are not seen.
+ *   lengths   device, [B] int32; positions from 2^31 - 256 on are not seen.
  *   mask      device, [T, words] uint64 (bits past the words are unset), or NULL.
  *   scale     finite.
  *   out       device, [T, q_heads, dim] in dtype, 16-byte aligned.

@@ -1612,7 +1612,7 @@ dresd_status attend_shape(const dresd_kv_cache *cache, int32_t q_heads, bool rag
   if (s != DRESD_OK) return s;
   if (q_heads < 1 || q_heads % p->c.heads)
     return fail(DRESD_EINVAL, "q_heads must be a multiple of the cache's heads");
-  if (B < 0) return fail(DRESD_EINVAL, "B must be >= 0");
+  if (B < 0 || B > (1 << 30) / p->c.heads) return fail(DRESD_EINVAL, "B out of range");
   if (T < 0 || T > 0x7fffffffLL / q_heads) return fail(DRESD_EINVAL, "T out of range");
   if (!ragged && (n < 0 || (int64_t)n * B != T)) return fail(DRESD_EINVAL, "T must be B n");
   if (width < 1) return fail(DRESD_EINVAL, "width must be >= 1");
