@@ -39,7 +39,7 @@ UNITS = [("dresd_kernels.hip", ["-DDRESD_TU=%d" % t], "kernels%d" % t) for t in 
     ("dresd_group.hip", [], "group"), ("dresd_layout.hip", [], "layout"),
     ("dresd_project.hip", [], "project"), ("dresd_bwprobe.hip", [], "bwprobe"),
     ("dresd_tree.hip", [], "tree"), ("dresd_kv.hip", [], "kv"),
-    ("dresd_attend.hip", [], "attend"),
+    ("dresd_attend.hip", [], "attend"), ("dresd_attend_tile.hip", [], "attendt"),
     ("dresd_attend_wave.hip", ["-DDRESD_ATTEND_DP=64"], "attendw64"),
     ("dresd_attend_wave.hip", ["-DDRESD_ATTEND_DP=128"], "attendw128"),
     ("dresd_attend_wave.hip", ["-DDRESD_ATTEND_DP=256"], "attendw256"),

@@ -197,6 +197,12 @@ __device__ __forceinline__ int reach(const AttendPlan &pl, const Unit &u, int ro
   return end < u.L ? (int)end : u.L;
 }
 
+// Positions that every row of the block sees, as far as there are pages.
+__device__ __forceinline__ int seen_by_all(const AttendPlan &pl, const Unit &u) {
+  const int64_t c = (int64_t)u.before + (pl.p.mask ? 0 : u.row0 / pl.group + 1);
+  return c < u.L ? (int)c : u.L;
+}
+
 // Which of the 64 positions from pos on the row of chunk token t sees, by the
 // length, the chunk and the mask.
 __device__ __forceinline__ uint64_t window(const AttendPlan &pl, const Unit &u, int64_t row, int t,

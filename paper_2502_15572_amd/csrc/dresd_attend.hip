@@ -31,14 +31,16 @@ namespace {
 constexpr int kSplitsMax = 64;
 constexpr int kJoinThreads = 256;
 
-// Joins the parts of every row: one wave per row and head, four dims a lane.
+// Joins the parts of every row, a workgroup per row and head: its eight 32-lane groups
+// take every eighth part, four dims a lane (and the dims past 128 in a second
+// turn), and their sums meet in LDS.
 template <int QT>
 __global__ void __launch_bounds__(kJoinThreads) dresd_attend_join(AttendPlan pl) {
+  constexpr int G = kJoinThreads / 32;
+  __shared__ f4 part[G][32];
   const AttendParams &p = pl.p;
-  const int lane = threadIdx.x & 63;
-  const int64_t rows = p.T * p.q_heads;
-  const int64_t r = (int64_t)blockIdx.x * (kJoinThreads / kWaveSize) + threadIdx.x / kWaveSize;
-  if (r >= rows) return;
+  const int lane = threadIdx.x & 63, g = threadIdx.x / 32, j = threadIdx.x % 32;
+  const int64_t rows = p.T * p.q_heads, r = blockIdx.x;
   if (p.ragged) {            // rows outside the chunks have no parts
     const int64_t t = r / p.q_heads;
     if (t < p.starts[0] || t >= p.starts[p.B]) return;
@@ -53,16 +55,31 @@ __global__ void __launch_bounds__(kJoinThreads) dresd_attend_join(AttendPlan pl)
   float l = own.y * a;
 #pragma unroll
   for (int o = 1; o < kWaveSize; o <<= 1) l += __shfl_xor(l, o, kWaveSize);
-  const int d = lane * 4;
-  f4 x = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < pl.splits; ++s) {
-    const float w = __shfl(a, s, kWaveSize);
-    if (w == 0.f || d >= p.c.dim) continue;      // (w: the wave's; NaN parts have weight)
-    const f4 y = *reinterpret_cast<const f4 *>(pl.part_o + ((int64_t)s * rows + r) * p.c.dim + d);
+  for (int d0 = 0; d0 < p.c.dim; d0 += 128) {
+    const int d = d0 + 4 * j;
+    f4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] += y[i] * w;
+    for (int i = 0; i < kSplitsMax / G; ++i) {
+      const int s = G * i + g;
+      const float w = __shfl(a, s & 63, kWaveSize);
+      if (s < pl.splits && w != 0.f && d < p.c.dim) {  // (a part without weight has no sums)
+        const f4 y =
+            *reinterpret_cast<const f4 *>(pl.part_o + ((int64_t)s * rows + r) * p.c.dim + d);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] += y[e] * w;
+      }
+    }
+    part[g][j] = x;
+    __syncthreads();
+    if (g == 0 && d < p.c.dim) {
+#pragma unroll
+      for (int i = 1; i < G; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] += part[i][j][e];
+      finish_row<QT>(p, r, d, x, top, l);
+    }
+    __syncthreads();
   }
-  if (d < p.c.dim) finish_row<QT>(p, r, d, x, top, l);
 }
 
 AttendPlan plan_of(const AttendParams &p, int cus) {
@@ -72,11 +89,8 @@ AttendPlan plan_of(const AttendParams &p, int cus) {
   // rows of the longest chunk (of ragged chunks: were they all alike)
   const int64_t tokens = p.ragged ? (p.T + (p.B > 0 ? p.B : 1) - 1) / (p.B > 0 ? p.B : 1) : p.n;
   const int64_t rows = tokens * pl.group;
-  const bool wide = p.c.dim > 128;
-  if (rows <= 16) pl.ct = 1;
-  else if (rows <= 32 || wide) pl.ct = 2;
-  else pl.ct = 4;
-  pl.rows = 16 * pl.ct;
+  pl.ct = rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 && p.c.dim <= 128 ? 4 : 0;
+  pl.rows = pl.ct ? 16 * pl.ct : 128;
   pl.blocks = (int)(p.ragged ? p.T * pl.group / pl.rows + p.B
                              : (int64_t)p.B * ((rows + pl.rows - 1) / pl.rows));
   const int64_t units = (int64_t)pl.blocks * p.c.heads;
@@ -109,18 +123,16 @@ hipError_t launch_attend(const AttendParams &p, int cus, hipStream_t st) {
   pl.part_ml = pl.part_o + part_floats(pl) * p.c.dim;
   const bool f8 = p.c.dtype == kF8;
   const int dp = p.c.dim <= 64 ? 64 : p.c.dim <= 128 ? 128 : 256;
-  const AttendKernel k = attend_wave_kernel(p.dtype, f8, dp, pl.ct);
-  const size_t lds = attend_wave_lds(f8, dp, pl.ct);
-  if (!k) return hipErrorInvalidConfiguration;
+  const AttendKernel k = pl.ct ? attend_wave_kernel(p.dtype, f8, dp, pl.ct)
+                               : attend_tile_kernel(p.dtype, f8, dp);
+  const size_t lds = pl.ct ? attend_wave_lds(f8, dp, pl.ct) : attend_tile_lds(dp);
   void *args[] = {&pl};
   hipError_t e = hipLaunchKernel((const void *)k, dim3((unsigned)((pl.total + 7) / 8 * 8)),
                                  dim3(256), args, lds, st);
   if (e != hipSuccess || pl.splits == 1) return e;
-  const int64_t rows = p.T * p.q_heads, per = kJoinThreads / kWaveSize;
   const void *j = p.dtype == kF16 ? (const void *)dresd_attend_join<kF16>
                                   : (const void *)dresd_attend_join<kBF16>;
-  return hipLaunchKernel(j, dim3((unsigned)((rows + per - 1) / per)), dim3(kJoinThreads), args, 0,
-                         st);
+  return hipLaunchKernel(j, dim3((unsigned)(p.T * p.q_heads)), dim3(kJoinThreads), args, 0, st);
 }
 
 }  // namespace dresd

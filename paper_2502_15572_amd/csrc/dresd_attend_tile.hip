@@ -1,0 +1,340 @@
+// gfx950 attention of many rows over a paged cache: 128 rows (tokens times query
+// heads of one cache head) a workgroup, 32 a wave.
+//
+// What bounds it is the matrix cores, and beside them the exponentials: 128 rows do 128
+// multiply-adds per 16-bit value read.  The four waves share each tile of 64 keys and
+// values through LDS, two tiles deep: while one is computed the next is on its way
+// to registers, and is written to the other buffer before the tile's only barrier.
+//
+// Scores are formed transposed, S^T = K Q^T, with 32 x 32 x 16 instructions: a lane
+// holds one row (lane % 32) and half the keys, which is, keys in another order, the
+// operand of O^T = V^T P^T.  The weights never leave their registers, and a row's
+// statistics and rescaling are those of two lanes.  Keys are stored so that the 16
+// bytes that 16 lanes read at once lie in different banks, values so that the
+// transposed reads of 4 keys by 32 dims do.
+//
+// Running softmax: as in the wave kernel, a row's reference moves only when a score
+// passes it by kSlack.
+#include <type_traits>
+
+#include "dresd_attend.h"
+
+namespace dresd {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = 4;
+constexpr int kKeys = 64;
+
+// Of each wave: row offsets [keys] i64, factors of keys and values [keys] f32 each.
+constexpr size_t kWaveBytes = kKeys * 16;
+// Whether a key of the tile has a value that is not finite, two tiles.
+constexpr size_t kFlagBytes = 2 * kKeys;
+constexpr size_t tile_bytes(int dp) { return (size_t)kKeys * dp * 2; }
+
+template <int QT, bool F8, int DP>
+__global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) dresd_attend_tile(AttendPlan pl) {
+  typedef Half<QT> H;
+  typedef typename H::v8 v8;
+  typedef short s8v __attribute__((ext_vector_type(8)));
+  constexpr int KS = DP / 16;                     // 16-dim steps
+  constexpr int LR = F8 ? DP / 16 : DP / 8;       // lanes of a row in a load
+  constexpr int RP = kThreads / LR;               // rows of a load
+  constexpr int NP = kKeys / RP;                  // loads of a tile
+  extern __shared__ __align__(16) uint8_t lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+  const int col = lane & 31, half = lane >> 5;
+  Unit u;
+  if (!unit_of(pl, u)) return;
+  const AttendParams &p = pl.p;
+  const int D = p.c.dim;
+
+  uint8_t *kt = lds, *vt = lds + 2 * tile_bytes(DP);
+  uint8_t *mine = lds + 4 * tile_bytes(DP) + (size_t)wid * kWaveBytes;
+  int64_t *offs = reinterpret_cast<int64_t *>(mine);
+  float *kf = reinterpret_cast<float *>(offs + kKeys), *vf = kf + kKeys;
+  uint8_t *flags = lds + 4 * tile_bytes(DP) + kWaves * kWaveBytes;
+
+  // queries: operand of row 32 wid + col
+  v8 q[KS];
+  const float c2 = fabsf(p.scale) * 1.44269504088896341f;
+  int r = u.row0 + 32 * wid + col;
+  const bool real = r < u.rows;
+  r = real ? r : u.rows - 1;
+  const int tok = r / pl.group;
+  const int64_t row = u.token0 + tok;
+  const int head = u.head * pl.group + (r - tok * pl.group);
+  {
+    const uint32_t flip = p.scale < 0.f ? 0x80008000u : 0u;  // (-q) . k |scale|
+    const uint16_t *src = static_cast<const uint16_t *>(p.q) + row * p.q_row + head * p.q_head;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int d = 16 * s + 8 * half;
+      u4 x = {};
+      if (d < D) x = *reinterpret_cast<const u4 *>(src + d);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] ^= flip;
+      q[s] = __builtin_bit_cast(v8, x);
+    }
+  }
+  f16v acc[DP / 32];
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
+  float m = -3e38f, l = 0.f;
+
+  // this split's tiles
+  const int end = reach(pl, u, pl.rows);
+  const int tiles = end > 0 ? (end + kKeys - 1) / kKeys : 0;
+  const int per = (tiles + pl.splits - 1) / pl.splits;
+  const int64_t lo = (int64_t)u.split * per;
+  const int first = lo < tiles ? (int)lo : tiles;
+  const int last = first + per < tiles ? first + per : tiles;
+  const int plain = seen_by_all(pl, u);
+
+  const uint8_t *kbase = static_cast<const uint8_t *>(p.c.k);
+  const uint8_t *vbase = static_cast<const uint8_t *>(p.c.v);
+  const int row_bytes = F8 ? D : 2 * D;
+  const int32_t *table = p.table + (int64_t)u.b * p.width;
+  const int in_page = (1 << p.c.page_log) - 1;
+
+  // page of key `lane` of a tile
+  auto page_of = [&](int t) -> int {
+    if (t >= last) return -1;
+    const int pos = t * kKeys + lane;
+    return pos < u.L ? table[pos >> p.c.page_log] : -1;
+  };
+  // offsets of a tile's rows into the wave's LDS; which of its keys there are
+  uint32_t ke = 0, ve = 0;                        // their exponents
+  auto place = [&](int t, int page) -> uint64_t {
+    const bool ok = (uint32_t)page < (uint32_t)p.c.pages;
+    const int64_t at = ok ? ((((int64_t)page * p.c.heads + u.head) << p.c.page_log) +
+                             ((t * kKeys + lane) & in_page))
+                          : 0;
+    offs[lane] = at * row_bytes;
+    if constexpr (F8) {
+      ke = ok ? p.c.k_exp[at] : 127u;
+      ve = ok ? p.c.v_exp[at] : 127u;
+    }
+    wave_sync_lds();
+    return __ballot(ok);
+  };
+
+  u4 kr[NP], vr[NP];
+  const int sl = tid % LR, sr = tid / LR;         // 16 bytes of a row, row within a load
+  const int sd = 16 * sl < row_bytes ? 16 * sl : 0;  // (dims past the head: as in the wave kernel)
+  auto load16 = [&](const uint8_t *src) -> u4 {
+    if (F8 && (D & 8)) {                          // rows are 8-byte aligned
+      const u2 a = *reinterpret_cast<const u2 *>(src + sd);
+      const u2 b = *reinterpret_cast<const u2 *>(src + (sd + 8 < row_bytes ? sd + 8 : sd));
+      return u4{a[0], a[1], b[0], b[1]};
+    }
+    return *reinterpret_cast<const u4 *>(src + sd);
+  };
+  auto load = [&]() {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int64_t o = offs[RP * i + sr];
+      kr[i] = load16(kbase + o);
+      vr[i] = load16(vbase + o);
+    }
+  };
+  auto kchunk = [&](int buf, int k, int c) -> uint8_t * {
+    return kt + buf * tile_bytes(DP) + ((size_t)k * (DP / 8) + (c ^ (k & (DP == 64 ? 7 : 15)))) * 16;
+  };
+  auto vchunk = [&](int buf, int k, int c) -> uint8_t * {
+    return vt + buf * tile_bytes(DP) +
+           ((size_t)k * (DP / 8) + (c ^ ((DP == 64 ? (k >> 1) & 1 : k & 3) << 2))) * 16;
+  };
+  // a tile from registers into LDS; where not every row sees all of its keys, keys that
+  // are not there as zeros, and values that are not finite apart
+  auto store = [&](int buf, bool masked, uint64_t ok) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int k = RP * i + sr;
+      if constexpr (F8) {
+        *reinterpret_cast<v8 *>(kchunk(buf, k, 2 * sl)) = from_f8<QT>(u2{kr[i][0], kr[i][1]});
+        *reinterpret_cast<v8 *>(kchunk(buf, k, 2 * sl + 1)) = from_f8<QT>(u2{kr[i][2], kr[i][3]});
+        u4 x = __builtin_bit_cast(u4, from_f8<QT>(u2{vr[i][0], vr[i][1]}));
+        u4 y = __builtin_bit_cast(u4, from_f8<QT>(u2{vr[i][2], vr[i][3]}));
+        if (masked) {
+          if (!((ok >> k) & 1)) x = y = u4{};
+          const bool e = drop_nonfinite<QT>(x), f = drop_nonfinite<QT>(y);
+          const uint64_t w = __ballot(e || f);
+          if (sl == 0) flags[buf * kKeys + k] = ((w >> (lane & ~(LR - 1))) & ((1ull << LR) - 1)) != 0;
+        }
+        *reinterpret_cast<u4 *>(vchunk(buf, k, 2 * sl)) = x;
+        *reinterpret_cast<u4 *>(vchunk(buf, k, 2 * sl + 1)) = y;
+      } else {
+        *reinterpret_cast<u4 *>(kchunk(buf, k, sl)) = kr[i];
+        u4 x = vr[i];
+        if (masked) {
+          if (!((ok >> k) & 1)) x = u4{};
+          const uint64_t w = __ballot(drop_nonfinite<QT>(x));
+          if (sl == 0) flags[buf * kKeys + k] = ((w >> (lane & ~(LR - 1))) & ((1ull << LR) - 1)) != 0;
+        }
+        *reinterpret_cast<u4 *>(vchunk(buf, k, sl)) = x;
+      }
+    }
+    if constexpr (F8) {
+      kf[lane] = __uint_as_float(ke << 23) * c2;
+      vf[lane] = __uint_as_float(ve << 23);
+    }
+  };
+
+  auto compute = [&](auto is_masked, int buf, int t, uint64_t ok) {
+    constexpr bool MASKED = decltype(is_masked)::value;
+    f16v s[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
+#pragma unroll
+    for (int i = 0; i < KS; ++i)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const v8 k = *reinterpret_cast<const v8 *>(kchunk(buf, 32 * b + col, 2 * i + half));
+        s[b] = H::mfma32(k, q[i], s[b]);
+      }
+    // key of element i of block b: 32 b + 8 (i / 4) + 4 half + i % 4
+    uint64_t see = ~0ull, bad = 0;
+    if constexpr (MASKED) {
+      see = window(pl, u, row, tok, t * kKeys) & ok;
+      bad = __ballot(flags[buf * kKeys + lane] != 0);
+    }
+    float top = -3e38f;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int k0 = 32 * b + 8 * j + 4 * half;
+        f4 kfac, vfac;
+        if constexpr (F8) {
+          kfac = *reinterpret_cast<const f4 *>(kf + k0);
+          vfac = *reinterpret_cast<const f4 *>(vf + k0);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float x = s[b][4 * j + i] * (F8 ? kfac[i] : c2);
+          if constexpr (MASKED) {
+            const bool is = (see >> (k0 + i)) & 1;
+            x = is ? ((bad >> (k0 + i)) & 1 ? __builtin_nanf("") : x) : -__builtin_huge_valf();
+          }
+          s[b][4 * j + i] = x;
+          if constexpr (F8 && QT == kF16) {
+            // the largest weight is that of the value as it is stored
+            const int e = (int)(__float_as_uint(vfac[i]) >> 23) - 127;
+            x += (float)(e < -60 ? -60 : e > 20 ? 20 : e);
+          }
+          top = fmaxf(top, x);
+        }
+      }
+    if (__any(top > m + H::kSlack)) {
+      top = fmaxf(top, __shfl_xor(top, 32, kWaveSize));
+      const float mn = fmaxf(m, top);
+      const float a = exp2_hw(m - mn);
+      m = mn;
+      l *= a;
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] *= a;
+    }
+    const float ref = m - H::kBias;
+    float sum = 0.f;
+    v8 w[4];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int k0 = 32 * b + 8 * j + 4 * half;
+        f4 vfac;
+        if constexpr (F8) vfac = *reinterpret_cast<const f4 *>(vf + k0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float x = exp2_hw(s[b][4 * j + i] - ref);
+          sum += x;
+          if constexpr (F8) {
+            x *= vfac[i];
+            if constexpr (MASKED)
+              if (!((see >> (k0 + i)) & 1)) x = 0.f;
+          }
+          w[2 * b + j / 2][4 * (j & 1) + i] = H::round(x);
+        }
+      }
+    l += sum;
+    const int g = (lane >> 4) & 1, i16 = lane & 15, in = (i16 & 1) * 8;
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) {
+        const int k = 16 * kk + 4 * half + (i16 >> 2), c = 4 * d + 2 * g + ((i16 & 3) >> 1);
+        const s4v a = read_transposed(vchunk(buf, k, c) + in);
+        const s4v b = read_transposed(vchunk(buf, k + 8, c) + in);
+        const v8 x = __builtin_bit_cast(
+            v8, s8v{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
+        acc[d] = H::mfma32(x, w[kk], acc[d]);
+      }
+  };
+
+  if (first < last) {
+    uint64_t ok = place(first, page_of(first));
+    load();
+    int page = page_of(first + 1);
+    bool masked = (first + 1) * kKeys > plain || ok != ~0ull;
+    store(0, masked, ok);
+    __syncthreads();
+    for (int t = first; t < last; ++t) {
+      const int buf = (t - first) & 1;
+      const bool more = t + 1 < last;
+      uint64_t next_ok = 0;
+      bool next_masked = false;
+      if (more) {
+        next_ok = place(t + 1, page);
+        load();
+        page = page_of(t + 2);
+        next_masked = (t + 2) * kKeys > plain || next_ok != ~0ull;
+      }
+      if (masked) compute(std::true_type{}, buf, t, ok);
+      else compute(std::false_type{}, buf, t, ok);
+      if (more) store(buf ^ 1, next_masked, next_ok);
+      __syncthreads();
+      ok = next_ok;
+      masked = next_masked;
+    }
+  }
+
+  l += __shfl_xor(l, 32, kWaveSize);
+  if (!real) return;
+  const int64_t out = row * p.q_heads + head;
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int dim = 32 * d + 8 * j + 4 * half;
+      if (dim < D)
+        store_row<QT>(pl, u.split, out, dim,
+                      f4{acc[d][4 * j], acc[d][4 * j + 1], acc[d][4 * j + 2], acc[d][4 * j + 3]},
+                      m - H::kBias, l);
+    }
+}
+
+template <int QT, bool F8>
+AttendKernel pick(int dp) {
+  if (dp == 64) return dresd_attend_tile<QT, F8, 64>;
+  if (dp == 128) return dresd_attend_tile<QT, F8, 128>;
+  return dresd_attend_tile<QT, F8, 256>;
+}
+
+}  // namespace
+
+AttendKernel attend_tile_kernel(int qt, bool f8, int dp) {
+  if (qt == kF16) return f8 ? pick<kF16, true>(dp) : pick<kF16, false>(dp);
+  return f8 ? pick<kBF16, true>(dp) : pick<kBF16, false>(dp);
+}
+
+size_t attend_tile_lds(int dp) { return 4 * tile_bytes(dp) + kWaves * kWaveBytes + kFlagBytes; }
+
+}  // namespace dresd

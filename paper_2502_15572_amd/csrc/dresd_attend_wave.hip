@@ -358,11 +358,11 @@ __global__ void __launch_bounds__(kThreads, CT == 1 && DP <= 128 ? 2 : 1)
     load();
     int page = page_of(t + kWaves);
     const uint64_t whole = KT == 64 ? ~0ull : (1ull << KT) - 1;
-    const int plain = u.before < u.L ? u.before : u.L;
+    const int plain = seen_by_all(pl, u);
     for (; t < last; t += kWaves) {
       const int ahead = page_of(t + 2 * kWaves);
       uint64_t next_ok = 0;
-      // positions before the chunk, all there: every row sees them
+      // keys that are all there and that every row sees
       if ((t + 1) * KT <= plain && (ok & whole) == whole)
         compute(std::false_type{}, t, ok, t + kWaves, page, next_ok);
       else
