@@ -99,18 +99,31 @@ __device__ __forceinline__ s4v read_transposed(const uint8_t *lds) {
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Zeros in place of infinities and NaN; whether there were any.
-template <int QT>
+// Zeros in place of infinities and NaN among 16 bytes of a cache row; whether there
+// were any.
+template <int QT, bool F8>
 __device__ __forceinline__ bool drop_nonfinite(u4 &x) {
-  bool any = false;
+  uint32_t any = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const bool lo = (x[i] & Half<QT>::kInf) == Half<QT>::kInf;
-    const bool hi = ((x[i] >> 16) & Half<QT>::kInf) == Half<QT>::kInf;
-    any |= lo || hi;
-    x[i] = (lo ? 0u : x[i] & 0xffffu) | (hi ? 0u : x[i] & 0xffff0000u);
+    if constexpr (F8) {      // bytes of 7 ones: those that a carry into their sign shows
+      const uint32_t m = ((x[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+      any |= m;
+      x[i] &= ~((m >> 7) * 255u);
+    } else {
+      const uint32_t lo = (x[i] & Half<QT>::kInf) == Half<QT>::kInf ? 0xffffu : 0u;
+      const uint32_t hi = ((x[i] >> 16) & Half<QT>::kInf) == Half<QT>::kInf ? 0xffff0000u : 0u;
+      any |= lo | hi;
+      x[i] &= ~(lo | hi);
+    }
   }
-  return any;
+  return any != 0;
+}
+
+// Factor of a value row of an 8-bit cache.  Byte 255 is none: NaN for every row,
+// or, where some rows do not see it, 0 (and the rows that do get NaN scores).
+__device__ __forceinline__ float value_factor(uint32_t byte, bool masked) {
+  return byte != 255u ? __uint_as_float(byte << 23) : masked ? 0.f : __builtin_nanf("");
 }
 
 // Positions past this are not seen (a tile's stay inside 31 bits).

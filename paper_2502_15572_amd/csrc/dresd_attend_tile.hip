@@ -141,91 +141,107 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) dresd_attend_tile
       vr[i] = load16(vbase + o);
     }
   };
-  auto kchunk = [&](int buf, int k, int c) -> uint8_t * {
+  auto kchunk = [&](auto buf, int k, int c) -> uint8_t * {
     return kt + buf * tile_bytes(DP) + ((size_t)k * (DP / 8) + (c ^ (k & (DP == 64 ? 7 : 15)))) * 16;
   };
-  auto vchunk = [&](int buf, int k, int c) -> uint8_t * {
+  auto vchunk = [&](auto buf, int k, int c) -> uint8_t * {
     return vt + buf * tile_bytes(DP) +
            ((size_t)k * (DP / 8) + (c ^ ((DP == 64 ? (k >> 1) & 1 : k & 3) << 2))) * 16;
   };
   // a tile from registers into LDS; where not every row sees all of its keys, keys that
   // are not there as zeros, and values that are not finite apart
-  auto store = [&](int buf, bool masked, uint64_t ok) {
+  auto store = [&](auto buf, bool masked, uint64_t ok) {
+    if (masked) {
+      const uint64_t there = ok >> sr, none = F8 ? __ballot(ve == 255u) >> sr : 0ull;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        if (!((there >> (RP * i)) & 1)) vr[i] = u4{};
+        const uint64_t w = __ballot(drop_nonfinite<QT, F8>(vr[i])) >> (lane & ~(LR - 1));
+        if (sl == 0)
+          flags[buf * kKeys + RP * i + sr] =
+              (w & ((1ull << LR) - 1)) != 0 || ((none >> (RP * i)) & 1);
+      }
+    }
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int k = RP * i + sr;
       if constexpr (F8) {
         *reinterpret_cast<v8 *>(kchunk(buf, k, 2 * sl)) = from_f8<QT>(u2{kr[i][0], kr[i][1]});
         *reinterpret_cast<v8 *>(kchunk(buf, k, 2 * sl + 1)) = from_f8<QT>(u2{kr[i][2], kr[i][3]});
-        u4 x = __builtin_bit_cast(u4, from_f8<QT>(u2{vr[i][0], vr[i][1]}));
-        u4 y = __builtin_bit_cast(u4, from_f8<QT>(u2{vr[i][2], vr[i][3]}));
-        if (masked) {
-          if (!((ok >> k) & 1)) x = y = u4{};
-          const bool e = drop_nonfinite<QT>(x), f = drop_nonfinite<QT>(y);
-          const uint64_t w = __ballot(e || f);
-          if (sl == 0) flags[buf * kKeys + k] = ((w >> (lane & ~(LR - 1))) & ((1ull << LR) - 1)) != 0;
-        }
-        *reinterpret_cast<u4 *>(vchunk(buf, k, 2 * sl)) = x;
-        *reinterpret_cast<u4 *>(vchunk(buf, k, 2 * sl + 1)) = y;
+        *reinterpret_cast<v8 *>(vchunk(buf, k, 2 * sl)) = from_f8<QT>(u2{vr[i][0], vr[i][1]});
+        *reinterpret_cast<v8 *>(vchunk(buf, k, 2 * sl + 1)) = from_f8<QT>(u2{vr[i][2], vr[i][3]});
       } else {
         *reinterpret_cast<u4 *>(kchunk(buf, k, sl)) = kr[i];
-        u4 x = vr[i];
-        if (masked) {
-          if (!((ok >> k) & 1)) x = u4{};
-          const uint64_t w = __ballot(drop_nonfinite<QT>(x));
-          if (sl == 0) flags[buf * kKeys + k] = ((w >> (lane & ~(LR - 1))) & ((1ull << LR) - 1)) != 0;
-        }
-        *reinterpret_cast<u4 *>(vchunk(buf, k, sl)) = x;
+        *reinterpret_cast<u4 *>(vchunk(buf, k, sl)) = vr[i];
       }
     }
     if constexpr (F8) {
       kf[lane] = __uint_as_float(ke << 23) * c2;
-      vf[lane] = __uint_as_float(ve << 23);
+      vf[lane] = value_factor(ve, masked);
     }
   };
 
-  auto compute = [&](auto is_masked, int buf, int t, uint64_t ok) {
-    constexpr bool MASKED = decltype(is_masked)::value;
+  auto compute = [&](auto buf, int t, bool masked, uint64_t ok) {
     f16v s[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
+    // (keys are read kAhead steps before their product, no further: registers)
+    constexpr int kAhead = 2;
+    v8 kx[kAhead + 1][2];
 #pragma unroll
-    for (int i = 0; i < KS; ++i)
+    for (int i = 0; i < KS + kAhead; ++i) {
+      if (i < KS)
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+          kx[i % (kAhead + 1)][b] =
+              *reinterpret_cast<const v8 *>(kchunk(buf, 32 * b + col, 2 * i + half));
+      if (i >= kAhead)
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+          s[b] = H::mfma32(kx[(i - kAhead) % (kAhead + 1)][b], q[i - kAhead], s[b]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // in powers of two; key of element 4 j + i of block b: 32 b + 8 j + 4 half + i
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        f4 kfac;
+        if constexpr (F8) kfac = *reinterpret_cast<const f4 *>(kf + 32 * b + 8 * j + 4 * half);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[b][4 * j + i] *= F8 ? kfac[i] : c2;
+      }
+    if (masked) {
+      const uint64_t see = (window(pl, u, row, tok, t * kKeys) & ok) >> (4 * half);
+      const uint64_t bad = __ballot(flags[buf * kKeys + lane] != 0) >> (4 * half);
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const v8 k = *reinterpret_cast<const v8 *>(kchunk(buf, 32 * b + col, 2 * i + half));
-        s[b] = H::mfma32(k, q[i], s[b]);
+        const uint32_t is = (uint32_t)(see >> (32 * b)), no = (uint32_t)(bad >> (32 * b));
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int bit = 8 * (e / 4) + e % 4;
+          float x = s[b][e];
+          x = (no >> bit) & 1 ? __builtin_nanf("") : x;
+          s[b][e] = (is >> bit) & 1 ? x : -__builtin_huge_valf();
+        }
       }
-    // key of element i of block b: 32 b + 8 (i / 4) + 4 half + i % 4
-    uint64_t see = ~0ull, bad = 0;
-    if constexpr (MASKED) {
-      see = window(pl, u, row, tok, t * kKeys) & ok;
-      bad = __ballot(flags[buf * kKeys + lane] != 0);
     }
     float top = -3e38f;
 #pragma unroll
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int k0 = 32 * b + 8 * j + 4 * half;
-        f4 kfac, vfac;
-        if constexpr (F8) {
-          kfac = *reinterpret_cast<const f4 *>(kf + k0);
-          vfac = *reinterpret_cast<const f4 *>(vf + k0);
-        }
+        f4 vfac;
+        if constexpr (F8 && QT == kF16)
+          vfac = *reinterpret_cast<const f4 *>(vf + 32 * b + 8 * j + 4 * half);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float x = s[b][4 * j + i] * (F8 ? kfac[i] : c2);
-          if constexpr (MASKED) {
-            const bool is = (see >> (k0 + i)) & 1;
-            x = is ? ((bad >> (k0 + i)) & 1 ? __builtin_nanf("") : x) : -__builtin_huge_valf();
-          }
-          s[b][4 * j + i] = x;
+          float x = s[b][4 * j + i];
           if constexpr (F8 && QT == kF16) {
             // the largest weight is that of the value as it is stored
-            const int e = (int)(__float_as_uint(vfac[i]) >> 23) - 127;
+            const int e = (int)((__float_as_uint(vfac[i]) >> 23) & 255u) - 127;
             x += (float)(e < -60 ? -60 : e > 20 ? 20 : e);
           }
           top = fmaxf(top, x);
@@ -256,27 +272,32 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) dresd_attend_tile
         for (int i = 0; i < 4; ++i) {
           float x = exp2_hw(s[b][4 * j + i] - ref);
           sum += x;
-          if constexpr (F8) {
-            x *= vfac[i];
-            if constexpr (MASKED)
-              if (!((see >> (k0 + i)) & 1)) x = 0.f;
-          }
+          if constexpr (F8) x *= vfac[i];
           w[2 * b + j / 2][4 * (j & 1) + i] = H::round(x);
         }
       }
     l += sum;
     const int g = (lane >> 4) & 1, i16 = lane & 15, in = (i16 & 1) * 8;
+    constexpr int kV = 4 * (DP / 32), kVAhead = 4;
+    v8 vx[kVAhead + 1];
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk)
-#pragma unroll
-      for (int d = 0; d < DP / 32; ++d) {
+    for (int i = 0; i < kV + kVAhead; ++i) {
+      if (i < kV) {
+        const int kk = i / (DP / 32), d = i % (DP / 32);
         const int k = 16 * kk + 4 * half + (i16 >> 2), c = 4 * d + 2 * g + ((i16 & 3) >> 1);
         const s4v a = read_transposed(vchunk(buf, k, c) + in);
         const s4v b = read_transposed(vchunk(buf, k + 8, c) + in);
-        const v8 x = __builtin_bit_cast(
+        vx[i % (kVAhead + 1)] = __builtin_bit_cast(
             v8, s8v{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
-        acc[d] = H::mfma32(x, w[kk], acc[d]);
       }
+      if (i >= kVAhead) {
+        const int j = i - kVAhead;
+        acc[j % (DP / 32)] =
+            H::mfma32(vx[j % (kVAhead + 1)], w[j / (DP / 32)], acc[j % (DP / 32)]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
 
   if (first < last) {
@@ -284,10 +305,11 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) dresd_attend_tile
     load();
     int page = page_of(first + 1);
     bool masked = (first + 1) * kKeys > plain || ok != ~0ull;
-    store(0, masked, ok);
+    typedef std::integral_constant<int, 0> B0;
+    typedef std::integral_constant<int, 1> B1;
+    store(B0{}, masked, ok);
     __syncthreads();
-    for (int t = first; t < last; ++t) {
-      const int buf = (t - first) & 1;
+    auto step = [&](auto buf, int t) {
       const bool more = t + 1 < last;
       uint64_t next_ok = 0;
       bool next_masked = false;
@@ -297,12 +319,17 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) dresd_attend_tile
         page = page_of(t + 2);
         next_masked = (t + 2) * kKeys > plain || next_ok != ~0ull;
       }
-      if (masked) compute(std::true_type{}, buf, t, ok);
-      else compute(std::false_type{}, buf, t, ok);
-      if (more) store(buf ^ 1, next_masked, next_ok);
+      __builtin_amdgcn_sched_barrier(0);
+      compute(buf, t, masked, ok);
+      __builtin_amdgcn_sched_barrier(0);
+      if (more) store(std::integral_constant<int, 1 - decltype(buf)::value>{}, next_masked, next_ok);
       __syncthreads();
       ok = next_ok;
       masked = next_masked;
+    };
+    for (int t = first; t < last; t += 2) {
+      step(B0{}, t);
+      if (t + 1 < last) step(B1{}, t + 1);
     }
   }
 

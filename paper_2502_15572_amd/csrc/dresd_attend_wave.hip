@@ -184,9 +184,8 @@ __global__ void __launch_bounds__(kThreads, CT == 1 && DP <= 128 ? 2 : 1)
   };
 
   // one tile: its keys and values are in registers, ok its keys that there are
-  auto compute = [&](auto masked, int t, uint64_t ok, int next, int next_page,
+  auto compute = [&](int t, bool masked, uint64_t ok, int next, int next_page,
                      uint64_t &next_ok) {
-    constexpr bool MASKED = decltype(masked)::value;
     // scores, rows of keys x columns of query rows
     f4 s[CT][U][2];
 #pragma unroll
@@ -208,49 +207,41 @@ __global__ void __launch_bounds__(kThreads, CT == 1 && DP <= 128 ? 2 : 1)
           for (int c = 0; c < CT; ++c) s[c][g][h] = H::mfma16(k, q[c][i], s[c][g][h]);
         }
       }
+    // values into LDS; where not every row sees all keys, keys that are not there as zeros,
+    // and keys with a value that is not finite apart
+    uint64_t bad = 0;
+    if (masked) {
+      if constexpr (F8) bad = __ballot(lane < KT && ve == 255u);
+#pragma unroll
+      for (int g = 0; g < U; ++g)
+#pragma unroll
+        for (int i = 0; i < VR; ++i) {
+          constexpr int RL = 64 / VL;             // rows of a load
+          if (!(((ok >> vk) >> (32 * g + RL * i)) & 1)) vr[g][i] = u4{};
+          uint64_t w = __ballot(drop_nonfinite<QT, F8>(vr[g][i]));
+          while (w) {                             // rare
+            const int j = __ffsll((long long)w) - 1;
+            bad |= 1ull << (32 * g + RL * i + j / VL);
+            w &= w - 1;
+          }
+        }
+    }
     if constexpr (F8) {
       if (lane < KT) {
-        // in masked tiles a key that is not there counts for nothing
         kf[lane] = __uint_as_float(ke << 23) * c2;
-        vf[lane] = __uint_as_float(ve << 23);
+        vf[lane] = value_factor(ve, masked);
       }
     }
-    // values into LDS; in masked tiles rows that are not there as zeros, and keys with a value
-    // that is not finite apart, for the rows that do not see them
-    uint64_t bad = 0;
 #pragma unroll
     for (int g = 0; g < U; ++g)
 #pragma unroll
       for (int i = 0; i < VR; ++i) {
         const int k = 32 * g + (64 / VL) * i + vk;
         if constexpr (F8) {
-          v8 a = from_f8<QT>(u2{vr[g][i][0], vr[g][i][1]});
-          v8 b = from_f8<QT>(u2{vr[g][i][2], vr[g][i][3]});
-          u4 x = __builtin_bit_cast(u4, a), y = __builtin_bit_cast(u4, b);
-          if constexpr (MASKED) {
-            if (!((ok >> k) & 1)) x = y = u4{};
-            const bool e = drop_nonfinite<QT>(x), f = drop_nonfinite<QT>(y);
-            uint64_t w = __ballot(e || f);
-            while (w) {                           // rare
-              const int j = __ffsll((long long)w) - 1;
-              bad |= 1ull << (32 * g + (64 / VL) * i + j / VL);
-              w &= w - 1;
-            }
-          }
-          *reinterpret_cast<u4 *>(chunk(k, 2 * vl)) = x;
-          *reinterpret_cast<u4 *>(chunk(k, 2 * vl + 1)) = y;
+          *reinterpret_cast<v8 *>(chunk(k, 2 * vl)) = from_f8<QT>(u2{vr[g][i][0], vr[g][i][1]});
+          *reinterpret_cast<v8 *>(chunk(k, 2 * vl + 1)) = from_f8<QT>(u2{vr[g][i][2], vr[g][i][3]});
         } else {
-          u4 x = vr[g][i];
-          if constexpr (MASKED) {
-            if (!((ok >> k) & 1)) x = u4{};
-            uint64_t w = __ballot(drop_nonfinite<QT>(x));
-            while (w) {
-              const int j = __ffsll((long long)w) - 1;
-              bad |= 1ull << (32 * g + (64 / VL) * i + j / VL);
-              w &= w - 1;
-            }
-          }
-          *reinterpret_cast<u4 *>(chunk(k, vl)) = x;
+          *reinterpret_cast<u4 *>(chunk(k, vl)) = vr[g][i];
         }
       }
     wave_sync_lds();
@@ -275,9 +266,27 @@ __global__ void __launch_bounds__(kThreads, CT == 1 && DP <= 128 ? 2 : 1)
     v8 w[CT][U];
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
-      uint64_t see = ~0ull;
-      if constexpr (MASKED) {
-        see = window(pl, u, row[c], tok[c], t * KT) & ok;
+#pragma unroll
+      for (int g = 0; g < U; ++g)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[c][g][h][i] *= F8 ? kfac[g][h][i] : c2;
+      if (masked) {
+        const uint64_t see = (window(pl, u, row[c], tok[c], t * KT) & ok) >> (4 * kq);
+        const uint64_t inf = bad >> (4 * kq);
+#pragma unroll
+        for (int g = 0; g < U; ++g) {
+          const uint32_t is = (uint32_t)(see >> (32 * g)), no = (uint32_t)(inf >> (32 * g));
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float x = s[c][g][h][i];
+              x = (no >> (16 * h + i)) & 1 ? __builtin_nanf("") : x;
+              s[c][g][h][i] = (is >> (16 * h + i)) & 1 ? x : -__builtin_huge_valf();
+            }
+        }
       }
       float top = -3e38f;
 #pragma unroll
@@ -286,16 +295,10 @@ __global__ void __launch_bounds__(kThreads, CT == 1 && DP <= 128 ? 2 : 1)
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            float x = s[c][g][h][i] * (F8 ? kfac[g][h][i] : c2);
-            if constexpr (MASKED) {
-              const int k = 32 * g + 16 * h + 4 * kq + i;
-              const bool is = (see >> k) & 1;
-              x = is ? ((bad >> k) & 1 ? __builtin_nanf("") : x) : -__builtin_huge_valf();
-            }
-            s[c][g][h][i] = x;
+            float x = s[c][g][h][i];
             if constexpr (F8 && QT == kF16) {
               // the largest weight is that of the value as it is stored
-              const int e = (int)(__float_as_uint(vfac[g][h][i]) >> 23) - 127;
+              const int e = (int)((__float_as_uint(vfac[g][h][i]) >> 23) & 255u) - 127;
               x += (float)(e < -60 ? -60 : e > 20 ? 20 : e);
             }
             top = fmaxf(top, x);
@@ -322,13 +325,7 @@ __global__ void __launch_bounds__(kThreads, CT == 1 && DP <= 128 ? 2 : 1)
           for (int i = 0; i < 4; ++i) {
             float x = exp2_hw(s[c][g][h][i] - ref);
             sum += x;
-            if constexpr (F8) {
-              x *= vfac[g][h][i];
-              if constexpr (MASKED) {
-                const int k = 32 * g + 16 * h + 4 * kq + i;
-                if (!((see >> k) & 1)) x = 0.f;
-              }
-            }
+            if constexpr (F8) x *= vfac[g][h][i];
             w[c][g][4 * h + i] = H::round(x);
           }
       l[c] += sum;
@@ -363,10 +360,8 @@ __global__ void __launch_bounds__(kThreads, CT == 1 && DP <= 128 ? 2 : 1)
       const int ahead = page_of(t + 2 * kWaves);
       uint64_t next_ok = 0;
       // keys that are all there and that every row sees
-      if ((t + 1) * KT <= plain && (ok & whole) == whole)
-        compute(std::false_type{}, t, ok, t + kWaves, page, next_ok);
-      else
-        compute(std::true_type{}, t, ok, t + kWaves, page, next_ok);
+      const bool masked = (t + 1) * KT > plain || (ok & whole) != whole;
+      compute(t, masked, ok, t + kWaves, page, next_ok);
       ok = next_ok;
       page = ahead;
     }
