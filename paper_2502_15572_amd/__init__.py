@@ -10,6 +10,7 @@ current stream to it.
 from __future__ import annotations
 
 import ctypes
+import functools
 
 from . import _lib
 from ._lib import DresdError, K_MAX, NODES_MAX  # noqa: F401
@@ -363,41 +364,64 @@ def pack_drafts(tokens, r: int, length: int, eos: int = 0, out=None, stream=None
 # ---- batch verification: the forward over the drafts, around the model's weights -----------
 
 
+class _Here:
+    """The context of a call whose device is current and whose stream is the current one."""
+
+    def __enter__(self):
+        pass
+
+    def __exit__(self, *exc):
+        pass
+
+
+_HERE = _Here()
+
+
 def _on(stream, *tensors):
     """Context in which a call on these GPU tensors allocates and launches: their device, and
     ``stream`` (outputs and workspaces then belong to it, and a later call on it may reuse
     them)."""
-    import contextlib
-
     import torch
-    device = None
+    index = -1
     for t in tensors:
         if t is None:
             continue
-        if not t.is_cuda:
+        i = t.get_device()
+        if i < 0:
             raise TypeError("all inputs must be GPU tensors")
-        if device is None:
-            device = t.device
-        elif t.device != device:
+        if index < 0:
+            index = i
+        elif i != index:
             raise ValueError("all tensors must be on one device")
     if stream is not None:
-        if stream.device != device:
+        if stream.device.index != index:
             raise ValueError("the stream must be on the tensors' device")
         return torch.cuda.stream(stream)
-    if device.index != torch.cuda.current_device():
-        return torch.cuda.device(device)
-    return contextlib.nullcontext()
+    if index != torch.cuda.current_device():
+        return torch.cuda.device(index)
+    return _HERE
+
+
+def _current(t):
+    """Handle of the current stream of a tensor's device."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
 def _expect(name, t, dtype, *shape):
-    """A contiguous tensor of this type and shape (None: any size)."""
+    """A contiguous tensor of this type and shape."""
     if t.dtype != dtype:
         raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
-    if t.dim() != len(shape) or any(w is not None and n != w for n, w in zip(t.shape, shape)):
-        raise ValueError("%s must have shape %s, not %s"
-                         % (name, list("?" if w is None else w for w in shape), list(t.shape)))
+    if t.shape != shape:
+        raise ValueError("%s must have shape %s, not %s" % (name, list(shape), list(t.shape)))
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
+
+
+def _expect_dim(name, t, dim):
+    if t.dim() != dim:
+        raise ValueError("%s must have %d dimensions" % (name, dim))
+    return t.shape
 
 
 def _ptr(t):
@@ -423,8 +447,8 @@ def draft_tree(drafts, count, next_tok, nodes: int | None = None, eos: int = 0, 
     ``eos``, the parent -1, depth and mask 0."""
     import torch
     i32 = torch.int32
-    _expect("drafts", drafts, i32, None, None, None)
-    B, r, length = drafts.shape
+    B, r, length = _expect_dim("drafts", drafts, 3)
+    _expect("drafts", drafts, i32, B, r, length)
     _expect("count", count, i32, B)
     _expect("next_tok", next_tok, i32, B)
     N = min(NODES_MAX, 1 + r * max(0, length - 1)) if nodes is None else int(nodes)
@@ -433,12 +457,8 @@ def draft_tree(drafts, count, next_tok, nodes: int | None = None, eos: int = 0, 
     W = (N + 63) // 64
     with _on(stream, drafts, count, next_tok, *(out or ())):
         if out is None:
-            dev = drafts.device
-            out = (torch.empty((B, N), dtype=i32, device=dev),
-                   torch.empty((B, N), dtype=i32, device=dev),
-                   torch.empty((B, N), dtype=i32, device=dev),
-                   torch.empty((B, N, W), dtype=torch.int64, device=dev),
-                   torch.empty((B,), dtype=i32, device=dev))
+            out = (*drafts.new_empty((3, B, N)).unbind(),
+                   drafts.new_empty((B, N, W), dtype=torch.int64), drafts.new_empty((B,)))
         else:
             for name, t in zip(("token", "parent", "depth"), out):
                 _expect(name, t, i32, B, N)
@@ -446,7 +466,7 @@ def draft_tree(drafts, count, next_tok, nodes: int | None = None, eos: int = 0, 
             _expect("nodes", out[4], i32, B)
         _lib.check(_lib.load().dresd_draft_tree(
             drafts.data_ptr(), count.data_ptr(), next_tok.data_ptr(), B, r, length, int(eos), N,
-            *(t.data_ptr() for t in out), _stream_handle()))
+            *(t.data_ptr() for t in out), _current(drafts)))
     return tuple(out)
 
 
@@ -463,9 +483,9 @@ def _kv_cache(k_pages, v_pages, k_exp, v_exp):
     code = _CACHE_DTYPES.get(k_pages.dtype)
     if code is None:
         raise TypeError("a cache is float16, bfloat16 or float8_e4m3fn, not %s" % k_pages.dtype)
-    _expect("k_pages", k_pages, k_pages.dtype, None, None, None, None)
-    _expect("v_pages", v_pages, k_pages.dtype, *k_pages.shape)
-    P, H, page, D = k_pages.shape
+    P, H, page, D = _expect_dim("k_pages", k_pages, 4)
+    _expect("k_pages", k_pages, k_pages.dtype, P, H, page, D)
+    _expect("v_pages", v_pages, k_pages.dtype, P, H, page, D)
     if (code == _lib.F8) != (k_exp is not None) or (k_exp is None) != (v_exp is None):
         raise ValueError("an 8-bit cache has k_exp and v_exp, a 16-bit one neither")
     if k_exp is not None:
@@ -497,7 +517,7 @@ def kv_write(k, v, slots, k_pages, v_pages, k_exp=None, v_exp=None, stream=None)
     with _on(stream, k, v, slots, k_pages, v_pages, k_exp, v_exp):
         _lib.check(_lib.load().dresd_kv_write(
             cache, k.data_ptr(), _stride(k, 0), _stride(k, 1), v.data_ptr(), _stride(v, 0),
-            _stride(v, 1), _dtype_code(k), slots.data_ptr(), n, _stream_handle()))
+            _stride(v, 1), _dtype_code(k), slots.data_ptr(), n, _current(k)))
 
 
 def kv_read(slots, k_pages, v_pages, k_exp=None, v_exp=None, dtype=None, out=None, stream=None):
@@ -507,22 +527,31 @@ def kv_read(slots, k_pages, v_pages, k_exp=None, v_exp=None, dtype=None, out=Non
     which holds their values exactly)."""
     import torch
     cache = _kv_cache(k_pages, v_pages, k_exp, v_exp)
-    _expect("slots", slots, torch.int64, None)
-    n = int(slots.shape[0])
+    n, = _expect_dim("slots", slots, 1)
+    _expect("slots", slots, torch.int64, n)
     if dtype is None:
         dtype = torch.bfloat16 if cache.dtype == _lib.F8 else k_pages.dtype
     with _on(stream, slots, k_pages, v_pages, k_exp, v_exp, *(out or ())):
         if out is None:
             shape = (n, cache.heads, cache.dim)
-            out = (torch.empty(shape, dtype=dtype, device=slots.device),
-                   torch.empty(shape, dtype=dtype, device=slots.device))
+            out = (slots.new_empty(shape, dtype=dtype), slots.new_empty(shape, dtype=dtype))
         else:
             _expect("k", out[0], dtype, n, cache.heads, cache.dim)
             _expect("v", out[1], dtype, n, cache.heads, cache.dim)
         _lib.check(_lib.load().dresd_kv_read(
             cache, slots.data_ptr(), n, _dtype_code(out[0]), out[0].data_ptr(),
-            out[1].data_ptr(), _stream_handle()))
+            out[1].data_ptr(), _current(slots)))
     return tuple(out)
+
+
+@functools.lru_cache(maxsize=1024)
+def _attention_workspace(device, pages, page, heads, dim, dtype, q_heads, ragged, n, B, T, width):
+    """Bytes of workspace of a call of this shape (the device is current)."""
+    need = ctypes.c_int64()
+    _lib.check(_lib.load().dresd_paged_attention_workspace(
+        _lib.KvCache(None, None, None, None, pages, page, heads, dim, dtype), q_heads, ragged, n,
+        B, T, width, ctypes.byref(need)))
+    return need.value
 
 
 def paged_attention(q, k_pages, v_pages, table, lengths, starts=None, mask=None, k_exp=None,
@@ -544,9 +573,10 @@ def paged_attention(q, k_pages, v_pages, table, lengths, starts=None, mask=None,
     that sees nothing).  ``out``: the output tensor, or the pair."""
     import torch
     cache = _kv_cache(k_pages, v_pages, k_exp, v_exp)
-    B = int(lengths.shape[0]) if lengths.dim() == 1 else -1
-    _expect("lengths", lengths, torch.int32, None)
-    _expect("table", table, torch.int32, B, None)
+    B, = _expect_dim("lengths", lengths, 1)
+    width = _expect_dim("table", table, 2)[1]
+    _expect("lengths", lengths, torch.int32, B)
+    _expect("table", table, torch.int32, B, width)
     if q.dtype not in (torch.float16, torch.bfloat16):
         raise TypeError("q must be float16 or bfloat16, not %s" % q.dtype)
     if starts is None:
@@ -566,17 +596,16 @@ def paged_attention(q, k_pages, v_pages, table, lengths, starts=None, mask=None,
         raise ValueError("q's last dimension must be %d contiguous elements" % cache.dim)
     words = 0
     if mask is not None:
-        _expect("mask", mask, torch.int64, *q.shape[:-2], None)
-        words = int(mask.shape[-1])
+        words = _expect_dim("mask", mask, q.dim() - 1)[-1]
+        _expect("mask", mask, torch.int64, *q.shape[:-2], words)
     if scale is None:
         scale = cache.dim ** -0.5
     given = out if isinstance(out, (tuple, list)) else () if out is None else (out,)
     lib = _lib.load()
     with _on(stream, q, k_pages, v_pages, k_exp, v_exp, table, lengths, starts, mask, *given):
         if not given:
-            o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device) \
-                if with_lse else None
+            o = q.new_empty(q.shape)
+            lse = q.new_empty(q.shape[:-1], dtype=torch.float32) if with_lse else None
         else:
             o, lse = given[0], given[1] if len(given) > 1 else None
             if (lse is not None) != with_lse:
@@ -584,14 +613,13 @@ def paged_attention(q, k_pages, v_pages, table, lengths, starts=None, mask=None,
             _expect("out", o, q.dtype, *q.shape)
             if lse is not None:
                 _expect("lse", lse, torch.float32, *q.shape[:-1])
-        need = ctypes.c_int64()
-        _lib.check(lib.dresd_paged_attention_workspace(
-            cache, H, starts is not None, n, B, T, int(table.shape[1]), ctypes.byref(need)))
-        work = torch.empty(need.value, dtype=torch.uint8, device=q.device) if need.value else None
+        need = _attention_workspace(q.get_device(), cache.pages, cache.page_size, cache.heads,
+                                    cache.dim, cache.dtype, H, starts is not None, n, B, T, width)
+        work = q.new_empty((need,), dtype=torch.uint8) if need else None
         _lib.check(lib.dresd_paged_attention(
             cache, q.data_ptr(), row, _stride(q, -2), _dtype_code(q), H, _ptr(starts), n, B, T,
-            table.data_ptr(), int(table.shape[1]), lengths.data_ptr(), _ptr(mask), words,
-            float(scale), o.data_ptr(), _ptr(lse), _ptr(work), need.value, _stream_handle()))
+            table.data_ptr(), width, lengths.data_ptr(), _ptr(mask), words, float(scale),
+            o.data_ptr(), _ptr(lse), _ptr(work), need, _current(q)))
     return (o, lse) if with_lse else o
 
 
@@ -617,10 +645,7 @@ def accept_drafts(logits, token, parent, nodes, most: int | None = None, out=Non
     most = N if most is None else int(most)
     with _on(stream, logits, token, parent, nodes, *(out or ())):
         if out is None:
-            dev = logits.device
-            out = (torch.empty((B, most), dtype=i32, device=dev),
-                   torch.empty((B,), dtype=i32, device=dev),
-                   torch.empty((B,), dtype=i32, device=dev))
+            out = (token.new_empty((B, most)), *token.new_empty((2, B)).unbind())
         else:
             _expect("path", out[0], i32, B, most)
             _expect("accepted", out[1], i32, B)
@@ -628,7 +653,7 @@ def accept_drafts(logits, token, parent, nodes, most: int | None = None, out=Non
         _lib.check(_lib.load().dresd_accept_drafts(
             logits.data_ptr(), _dtype_code(logits), max(row, V), V, token.data_ptr(),
             parent.data_ptr(), nodes.data_ptr(), B, N, most, *(t.data_ptr() for t in out),
-            _stream_handle()))
+            _current(logits)))
     return tuple(out)
 
 

@@ -120,6 +120,12 @@ __device__ __forceinline__ bool drop_nonfinite(u4 &x) {
   return any != 0;
 }
 
+// From a product q . k (or (-q) . k, for a negative scale) to powers of two.  Never 0,
+// so that a masked score stays -inf.
+__device__ __forceinline__ float score_factor(float scale) {
+  return fmaxf(fabsf(scale) * 1.44269504088896341f, 1e-30f);
+}
+
 // Factor of a value row of an 8-bit cache.  Byte 255 is none: NaN for every row,
 // or, where some rows do not see it, 0 (and the rows that do get NaN scores).
 __device__ __forceinline__ float value_factor(uint32_t byte, bool masked) {

@@ -13,6 +13,7 @@
 // matrix operand, so grouped heads read the cache once.  Up to 64 rows: the wave
 // kernel (dresd_attend_wave.hip), whose waves stream the keys each for itself;
 // more: the tile kernel (dresd_attend_tile.hip), whose waves share them.
+#include <stdlib.h>
 #include "dresd_attend.h"
 
 namespace dresd {
@@ -31,37 +32,47 @@ namespace {
 constexpr int kSplitsMax = 64;
 constexpr int kJoinThreads = 256;
 
-// Joins the parts of every row, a workgroup per row and head: its eight 32-lane groups
-// take every eighth part, four dims a lane (and the dims past 128 in a second
-// turn), and their sums meet in LDS.
-template <int QT>
+// Joins the parts of every row and head: `GS` 32-lane groups of a workgroup a row, of
+// which each takes every GS-th part, four dims a lane (the dims past 128 in a second
+// turn), and whose sums meet in LDS.
+template <int QT, int GS>
 __global__ void __launch_bounds__(kJoinThreads) dresd_attend_join(AttendPlan pl) {
   constexpr int G = kJoinThreads / 32;
   __shared__ f4 part[G][32];
   const AttendParams &p = pl.p;
-  const int lane = threadIdx.x & 63, g = threadIdx.x / 32, j = threadIdx.x % 32;
-  const int64_t rows = p.T * p.q_heads, r = blockIdx.x;
-  if (p.ragged) {            // rows outside the chunks have no parts
+  const int g = threadIdx.x / 32, j = threadIdx.x % 32, gs = g % GS;
+  const int64_t rows = p.T * p.q_heads, r = (int64_t)blockIdx.x * (G / GS) + g / GS;
+  bool real = r < rows;
+  if (real && p.ragged) {    // rows outside the chunks have no parts
     const int64_t t = r / p.q_heads;
-    if (t < p.starts[0] || t >= p.starts[p.B]) return;
+    real = t >= p.starts[0] && t < p.starts[p.B];
   }
   const float2 *ml = reinterpret_cast<const float2 *>(pl.part_ml);
-  float2 own = {-3e38f, 0.f};                    // lane s: part s
-  if (lane < pl.splits) own = ml[(int64_t)lane * rows + r];
-  float top = own.x;
+  float2 own[2];                                 // parts j and j + 32
+  float top = -3e38f, l = 0.f;
 #pragma unroll
-  for (int o = 1; o < kWaveSize; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, kWaveSize));
-  const float a = own.y != 0.f ? exp2_hw(own.x - top) : 0.f;
-  float l = own.y * a;
+  for (int i = 0; i < 2; ++i) {
+    own[i] = real && j + 32 * i < pl.splits ? ml[(int64_t)(j + 32 * i) * rows + r]
+                                            : float2{-3e38f, 0.f};
+    top = fmaxf(top, own[i].x);
+  }
 #pragma unroll
-  for (int o = 1; o < kWaveSize; o <<= 1) l += __shfl_xor(l, o, kWaveSize);
+  for (int o = 1; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 32));
+  float a[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    a[i] = own[i].y != 0.f ? exp2_hw(own[i].x - top) : 0.f;
+    l += own[i].y * a[i];
+  }
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) l += __shfl_xor(l, o, 32);
   for (int d0 = 0; d0 < p.c.dim; d0 += 128) {
     const int d = d0 + 4 * j;
     f4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < kSplitsMax / G; ++i) {
-      const int s = G * i + g;
-      const float w = __shfl(a, s & 63, kWaveSize);
+    for (int i = 0; i < (GS == G ? kSplitsMax / G : 1); ++i) {
+      const int s = GS * i + gs;
+      const float w = __shfl(i < 32 / GS ? a[0] : a[1], s & 31, 32);
       if (s < pl.splits && w != 0.f && d < p.c.dim) {  // (a part without weight has no sums)
         const f4 y =
             *reinterpret_cast<const f4 *>(pl.part_o + ((int64_t)s * rows + r) * p.c.dim + d);
@@ -71,15 +82,22 @@ __global__ void __launch_bounds__(kJoinThreads) dresd_attend_join(AttendPlan pl)
     }
     part[g][j] = x;
     __syncthreads();
-    if (g == 0 && d < p.c.dim) {
+    if (real && gs == 0 && d < p.c.dim) {
 #pragma unroll
-      for (int i = 1; i < G; ++i)
+      for (int i = 1; i < GS; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] += part[i][j][e];
+        for (int e = 0; e < 4; ++e) x[e] += part[g + i][j][e];
       finish_row<QT>(p, r, d, x, top, l);
     }
     __syncthreads();
   }
+}
+
+template <int QT>
+const void *join_kernel(int groups) {
+  return groups == 2   ? (const void *)dresd_attend_join<QT, 2>
+         : groups == 4 ? (const void *)dresd_attend_join<QT, 4>
+                       : (const void *)dresd_attend_join<QT, 8>;
 }
 
 AttendPlan plan_of(const AttendParams &p, int cus) {
@@ -97,7 +115,8 @@ AttendPlan plan_of(const AttendParams &p, int cus) {
   // Enough workgroups for every compute unit to hold several, but none without a
   // round of tiles.
   const int64_t room = (int64_t)p.width << p.c.page_log;
-  int64_t s = units > 0 ? (4 * (int64_t)cus + units - 1) / units : 1;
+  static const int tw = getenv("TW") ? atoi(getenv("TW")) : 4, tt = getenv("TT") ? atoi(getenv("TT")) : 4;
+  int64_t s = units > 0 ? ((pl.ct ? tw : tt) * (int64_t)cus + units - 1) / units : 1;
   const int64_t most = (room + 127) / 128;
   s = s < most ? s : most;
   pl.splits = (int)(s < 1 ? 1 : s < kSplitsMax ? s : kSplitsMax);
@@ -130,9 +149,12 @@ hipError_t launch_attend(const AttendParams &p, int cus, hipStream_t st) {
   hipError_t e = hipLaunchKernel((const void *)k, dim3((unsigned)((pl.total + 7) / 8 * 8)),
                                  dim3(256), args, lds, st);
   if (e != hipSuccess || pl.splits == 1) return e;
-  const void *j = p.dtype == kF16 ? (const void *)dresd_attend_join<kF16>
-                                  : (const void *)dresd_attend_join<kBF16>;
-  return hipLaunchKernel(j, dim3((unsigned)(p.T * p.q_heads)), dim3(kJoinThreads), args, 0, st);
+  // up to 8 parts are read at once
+  const int groups = pl.splits <= 2 ? 2 : pl.splits <= 4 ? 4 : 8;
+  const void *j = p.dtype == kF16 ? join_kernel<kF16>(groups) : join_kernel<kBF16>(groups);
+  const int64_t rows = p.T * p.q_heads, per = kJoinThreads / 32 / groups;
+  return hipLaunchKernel(j, dim3((unsigned)((rows + per - 1) / per)), dim3(kJoinThreads), args, 0,
+                         st);
 }
 
 }  // namespace dresd

@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) dresd_attend_tile
 
   // queries: operand of row 32 wid + col
   v8 q[KS];
-  const float c2 = fabsf(p.scale) * 1.44269504088896341f;
+  const float c2 = score_factor(p.scale);
   int r = u.row0 + 32 * wid + col;
   const bool real = r < u.rows;
   r = real ? r : u.rows - 1;
@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) dresd_attend_tile
       }
     }
     if constexpr (F8) {
-      kf[lane] = __uint_as_float(ke << 23) * c2;
+      kf[lane] = __uint_as_float(ke << 23);
       vf[lane] = value_factor(ve, masked);
     }
   };
@@ -188,6 +188,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) dresd_attend_tile
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
     // (keys are read kAhead steps before their product, no further: registers)
+    __builtin_amdgcn_s_setprio(1);
     constexpr int kAhead = 2;
     v8 kx[kAhead + 1][2];
 #pragma unroll
@@ -203,16 +204,17 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) dresd_attend_tile
           s[b] = H::mfma32(kx[(i - kAhead) % (kAhead + 1)][b], q[i - kAhead], s[b]);
       __builtin_amdgcn_sched_barrier(0);
     }
-    // in powers of two; key of element 4 j + i of block b: 32 b + 8 j + 4 half + i
+    __builtin_amdgcn_s_setprio(0);
+    // key of element 4 j + i of block b: 32 b + 8 j + 4 half + i
+    if constexpr (F8)
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        f4 kfac;
-        if constexpr (F8) kfac = *reinterpret_cast<const f4 *>(kf + 32 * b + 8 * j + 4 * half);
+        for (int j = 0; j < 4; ++j) {
+          const f4 kfac = *reinterpret_cast<const f4 *>(kf + 32 * b + 8 * j + 4 * half);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[b][4 * j + i] *= F8 ? kfac[i] : c2;
-      }
+          for (int i = 0; i < 4; ++i) s[b][4 * j + i] *= kfac[i];
+        }
     if (masked) {
       const uint64_t see = (window(pl, u, row, tok, t * kKeys) & ok) >> (4 * half);
       const uint64_t bad = __ballot(flags[buf * kKeys + lane] != 0) >> (4 * half);
@@ -242,11 +244,12 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) dresd_attend_tile
           if constexpr (F8 && QT == kF16) {
             // the largest weight is that of the value as it is stored
             const int e = (int)((__float_as_uint(vfac[i]) >> 23) & 255u) - 127;
-            x += (float)(e < -60 ? -60 : e > 20 ? 20 : e);
+            x = x * c2 + (float)(e < -60 ? -60 : e > 20 ? 20 : e);
           }
           top = fmaxf(top, x);
         }
       }
+    if constexpr (!(F8 && QT == kF16)) top *= c2;  // (in powers of two)
     if (__any(top > m + H::kSlack)) {
       top = fmaxf(top, __shfl_xor(top, 32, kWaveSize));
       const float mn = fmaxf(m, top);
@@ -270,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) dresd_attend_tile
         if constexpr (F8) vfac = *reinterpret_cast<const f4 *>(vf + k0);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float x = exp2_hw(s[b][4 * j + i] - ref);
+          float x = exp2_hw(fmaf(s[b][4 * j + i], c2, -ref));
           sum += x;
           if constexpr (F8) x *= vfac[i];
           w[2 * b + j / 2][4 * (j & 1) + i] = H::round(x);
@@ -278,6 +281,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) dresd_attend_tile
       }
     l += sum;
     const int g = (lane >> 4) & 1, i16 = lane & 15, in = (i16 & 1) * 8;
+    __builtin_amdgcn_s_setprio(1);
     constexpr int kV = 4 * (DP / 32), kVAhead = 4;
     v8 vx[kVAhead + 1];
     __builtin_amdgcn_sched_barrier(0);
@@ -298,6 +302,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) dresd_attend_tile
       }
       __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(0);
   };
 
   if (first < last) {

@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(kThreads, CT == 1 && DP <= 128 ? 2 : 1)
   int tok[CT];
   int64_t row[CT];
   const uint32_t flip = p.scale < 0.f ? 0x80008000u : 0u;  // (-q) . k |scale|
-  const float c2 = fabsf(p.scale) * 1.44269504088896341f;
+  const float c2 = score_factor(p.scale);
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
     int r = u.row0 + 16 * c + col;
@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(kThreads, CT == 1 && DP <= 128 ? 2 : 1)
     }
     if constexpr (F8) {
       if (lane < KT) {
-        kf[lane] = __uint_as_float(ke << 23) * c2;
+        kf[lane] = __uint_as_float(ke << 23);
         vf[lane] = value_factor(ve, masked);
       }
     }
@@ -266,12 +266,13 @@ __global__ void __launch_bounds__(kThreads, CT == 1 && DP <= 128 ? 2 : 1)
     v8 w[CT][U];
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
+      if constexpr (F8)
 #pragma unroll
-      for (int g = 0; g < U; ++g)
+        for (int g = 0; g < U; ++g)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[c][g][h][i] *= F8 ? kfac[g][h][i] : c2;
+            for (int i = 0; i < 4; ++i) s[c][g][h][i] *= kfac[g][h][i];
       if (masked) {
         const uint64_t see = (window(pl, u, row[c], tok[c], t * KT) & ok) >> (4 * kq);
         const uint64_t inf = bad >> (4 * kq);
@@ -299,10 +300,11 @@ __global__ void __launch_bounds__(kThreads, CT == 1 && DP <= 128 ? 2 : 1)
             if constexpr (F8 && QT == kF16) {
               // the largest weight is that of the value as it is stored
               const int e = (int)((__float_as_uint(vfac[g][h][i]) >> 23) & 255u) - 127;
-              x += (float)(e < -60 ? -60 : e > 20 ? 20 : e);
+              x = x * c2 + (float)(e < -60 ? -60 : e > 20 ? 20 : e);
             }
             top = fmaxf(top, x);
           }
+      if constexpr (!(F8 && QT == kF16)) top *= c2;  // (in powers of two)
       if (__any(top > m[c] + H::kSlack)) {
         top = fmaxf(top, __shfl_xor(top, 16, kWaveSize));
         top = fmaxf(top, __shfl_xor(top, 32, kWaveSize));
@@ -323,7 +325,7 @@ __global__ void __launch_bounds__(kThreads, CT == 1 && DP <= 128 ? 2 : 1)
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            float x = exp2_hw(s[c][g][h][i] - ref);
+            float x = exp2_hw(fmaf(s[c][g][h][i], c2, -ref));
             sum += x;
             if constexpr (F8) x *= vfac[g][h][i];
             w[c][g][4 * h + i] = H::round(x);
