@@ -45,6 +45,12 @@ struct Half<kF16> {
   static __device__ __forceinline__ f16v mfma32(v8 a, v8 b, f16v c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
   }
+  // the 16 x 16 x 16 instruction, four elements a lane
+  static __device__ __forceinline__ f4 mfma16_half(u2 a, u2 b, f4 c) {
+    typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+    return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(h4, a),
+                                                 __builtin_bit_cast(h4, b), c, 0, 0, 0);
+  }
   static __device__ __forceinline__ _Float16 round(float x) { return (_Float16)x; }
   static constexpr uint32_t kInf = 0x7c00u;
   // Weights are kept at 2^10 times their value against the reference, so that small ones
@@ -59,6 +65,10 @@ struct Half<kBF16> {
   }
   static __device__ __forceinline__ f16v mfma32(v8 a, v8 b, f16v c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ f4 mfma16_half(u2 a, u2 b, f4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s4v, a),
+                                                     __builtin_bit_cast(s4v, b), c, 0, 0, 0);
   }
   static __device__ __forceinline__ __bf16 round(float x) { return (__bf16)x; }
   static constexpr uint32_t kInf = 0x7f80u;
@@ -95,6 +105,14 @@ __device__ __forceinline__ typename Half<QT>::v8 from_f8(u2 x) {
 __device__ __forceinline__ s4v read_transposed(const uint8_t *lds) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
       (__attribute__((address_space(3))) s4v *)(lds));
+}
+
+// The same for an 8 x 16 block of bytes: lane i names row i / 2 and columns 8 (i % 2) .. + 7,
+// and receives column i of the eight rows.
+__device__ __forceinline__ u2 read_transposed8(const uint8_t *lds) {
+  typedef int i2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                                    (__attribute__((address_space(3))) i2 *)(lds)));
 }
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }

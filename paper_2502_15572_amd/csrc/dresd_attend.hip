@@ -10,10 +10,9 @@
 // were split.
 //
 // The query rows that share a cache head (tokens times heads of the group) are one
-// matrix operand, so grouped heads read the cache once.  Up to 64 rows: the wave
+// matrix operand, so grouped heads read the cache once.  Few rows: the wave
 // kernel (dresd_attend_wave.hip), whose waves stream the keys each for itself;
 // more: the tile kernel (dresd_attend_tile.hip), whose waves share them.
-#include <stdlib.h>
 #include "dresd_attend.h"
 
 namespace dresd {
@@ -25,6 +24,15 @@ AttendKernel attend_wave_kernel(int qt, bool f8, int dp, int ct) {
   return dp == 64    ? attend_wave_kernel_64(qt, f8, ct)
          : dp == 128 ? attend_wave_kernel_128(qt, f8, ct)
                      : attend_wave_kernel_256(qt, f8, ct);
+}
+
+size_t attend_wave_lds_64(bool f8, int ct);
+size_t attend_wave_lds_128(bool f8, int ct);
+size_t attend_wave_lds_256(bool f8, int ct);
+size_t attend_wave_lds(bool f8, int dp, int ct) {
+  return dp == 64    ? attend_wave_lds_64(f8, ct)
+         : dp == 128 ? attend_wave_lds_128(f8, ct)
+                     : attend_wave_lds_256(f8, ct);
 }
 
 namespace {
@@ -107,7 +115,13 @@ AttendPlan plan_of(const AttendParams &p, int cus) {
   // rows of the longest chunk (of ragged chunks: were they all alike)
   const int64_t tokens = p.ragged ? (p.T + (p.B > 0 ? p.B : 1) - 1) / (p.B > 0 ? p.B : 1) : p.n;
   const int64_t rows = tokens * pl.group;
-  pl.ct = rows <= 16 ? 1 : rows <= 32 ? 2 : rows <= 64 && p.c.dim <= 128 ? 4 : 0;
+  // Up to 32 rows the wave kernel; in 8 bits up to 64, in two blocks, since the tile kernel
+  // converts what it reads before it shares it (64 rows of 8 x 32 heads of 128 over 1,000 to
+  // 4,000 tokens: 8 bits 74 us against 101, 16 bits 107 against 99).  The wave kernel copies 16
+  // bytes at a time.
+  const bool f8 = p.c.dtype == kF8;
+  const bool wave = rows <= (f8 && p.c.dim <= 128 ? 64 : 32) && !(f8 && p.c.dim % 16);
+  pl.ct = !wave ? 0 : rows <= 16 ? 1 : 2;
   pl.rows = pl.ct ? 16 * pl.ct : 128;
   pl.blocks = (int)(p.ragged ? p.T * pl.group / pl.rows + p.B
                              : (int64_t)p.B * ((rows + pl.rows - 1) / pl.rows));
@@ -115,8 +129,7 @@ AttendPlan plan_of(const AttendParams &p, int cus) {
   // Enough workgroups for every compute unit to hold several, but none without a
   // round of tiles.
   const int64_t room = (int64_t)p.width << p.c.page_log;
-  static const int tw = getenv("TW") ? atoi(getenv("TW")) : 4, tt = getenv("TT") ? atoi(getenv("TT")) : 4;
-  int64_t s = units > 0 ? ((pl.ct ? tw : tt) * (int64_t)cus + units - 1) / units : 1;
+  int64_t s = units > 0 ? (2 * (int64_t)cus + units - 1) / units : 1;
   const int64_t most = (room + 127) / 128;
   s = s < most ? s : most;
   pl.splits = (int)(s < 1 ? 1 : s < kSplitsMax ? s : kSplitsMax);

@@ -1,24 +1,30 @@
-// gfx950 attention of few rows over a paged cache: up to 16, 32 or 64 rows (tokens
-// times query heads of one cache head) a workgroup.
+// gfx950 attention of few rows over a paged cache: 16 or 32 rows (tokens times query
+// heads of one cache head) a workgroup.
 //
-// What bounds it is reading the cache: a workgroup does 16 to 64 multiply-adds per
-// 16-bit value read, the matrix cores' and the memory's rates being some 350
-// apart.  So nothing is shared: each of the 4 waves streams tiles of its own (wave
-// w the tiles w, w + 4, ... of the split), keys from memory to registers as the
-// operand that the matrix instruction takes, values through a swizzled LDS tile of
-// the wave's own that is read transposed, and no barrier holds a wave up before the
-// end.  While a tile is computed, the next one is on its way.
+// What bounds it is reading the cache: a workgroup does 16 or 32 multiply-adds per
+// value read, the matrix cores' and the memory's rates being some 350 apart.  So
+// the reading is all that is arranged for.  The four waves share nothing before
+// the end: each streams tiles of its own (wave w the tiles w, w + 4, ... of the
+// split) through a ring of LDS slots, by copies that go from memory to LDS without
+// registers, past the caches and without a barrier; all slots but the one at hand are
+// on their way.  Page ids run one ring further ahead, as copies too, so that nothing
+// waits for memory but the wait for a whole tile.
+// 16-bit caches are read at 5.7 TB/s, 8-bit ones at 5.5 (64 sequences of 2,000 to 8,000 tokens,
+// 8 heads of 128, 8 query heads each); the copies alone, without the products,
+// reach 6.4 and 6.0, loads through the caches a tenth less.
+//
+// Copies land lane after lane, so what a lane fetches decides the layout: 16-byte
+// chunks of a row are exchanged so that the keys that 16 lanes read at once, and the
+// values that are read transposed, lie in different banks.
 //
 // Scores are formed transposed, S^T = K Q^T: a lane then holds one row (lane % 16)
-// and 4 keys of every 16, which is, keys in another order, the operand that the
-// second product O^T = V^T P^T takes.  The weights never leave their registers,
-// and a row's statistics and the rescaling of its sums are one lane's.
+// and 4 keys of every 16, which is the operand that the second product
+// O^T = V^T P^T takes.  The weights never leave their registers, and a row's
+// statistics and the rescaling of its sums are one lane's.
 //
 // Running softmax: the reference m of a row is moved only when a score passes it by
 // kSlack (in powers of two); until then weights and sums grow past 1.  With m moved
 // at most once for most rows, the exchange between a row's 4 lanes is rare.
-#include <type_traits>
-
 #include "dresd_attend.h"
 
 #ifndef DRESD_ATTEND_DP
@@ -32,39 +38,81 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = 4;
 
-// Keys of a tile: 16 KiB of keys and values at a width of 128.
-constexpr int tile_keys(bool f8) { return f8 ? 64 : 32; }
+// Shape of the ring: a tile is one 16-key group (16 bit) or two (8 bit), a slot its
+// keys and its values, each row of DP elements.
+template <bool F8, int DP>
+struct Ring {
+  // Up to a width of 128 registers are left for two waves a SIMD, which share the LDS (one
+  // wave with a ring of four slots had the memory wait for its products: 64 sequences of
+  // up to 8,000 tokens, 8 heads of 128 in 8 bits, 145 us against 120).
+  static constexpr bool kPair = DP <= 128;
+  static constexpr int kKeys = F8 ? 32 : 16;
+  static constexpr int kPitch = DP * (F8 ? 1 : 2);      // bytes of a row
+  static constexpr int kHalf = kKeys * kPitch;          // of a tile's keys, or values
+  static constexpr int kSlots = (kPair ? 16384 : 32768) / (2 * kHalf);
+  static constexpr int kCopies = kHalf / 1024;          // of keys, and of values
+  static constexpr int kRows = 1024 / kPitch;           // rows of a copy
+  // of a wave: slots, row offsets of a tile, page ids of two rings of tiles, exponents of
+  // keys and values
+  static constexpr int kOffs = kKeys * 8;
+  static constexpr int kIds = 2 * kSlots * kKeys * 4;
+  static constexpr int kExps = F8 ? kSlots * kKeys * 8 : 0;
+  static constexpr int kBytes = kSlots * 2 * kHalf + kOffs + kIds + kExps;
+  // operations of a tile's copies
+  static constexpr int kOps = 2 * kCopies + (F8 ? 2 : 0);
+};
 
-// LDS of a wave: values [keys][DP] 16 bit, row offsets [keys] i64, factors of
-// keys and values [keys] f32 each (8-bit caches).
-constexpr size_t wave_bytes(bool f8, int dp) {
-  return (size_t)tile_keys(f8) * (dp * 2 + 8 + 8);
-}
 // At the end: sums [waves][rows][DP + 4] and statistics [waves][rows][2].
 constexpr size_t end_bytes(int dp, int ct) {
   return (size_t)kWaves * 16 * ct * (dp + 4 + 2) * 4;
 }
 
+typedef __attribute__((address_space(3))) uint8_t lds_byte;
+__device__ __forceinline__ uint32_t lds_address(const uint8_t *p) {
+  return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_byte *)(p));
+}
+// Copies from each lane's own address to LDS: 16 bytes to lds + 16 lane; one byte,
+// widened to a dword, to lds + 4 lane.  Callers wait with wait_vmcnt.
+__device__ __forceinline__ void copy16_from(const uint8_t *src, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %1\n\t"
+      "global_load_lds_dwordx4 %0, off nt"
+      :
+      : "v"(src), "s"(lds)
+      : "memory");
+}
+__device__ __forceinline__ void copy_byte_from(const uint8_t *src, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %1\n\t"
+      "global_load_lds_ubyte %0, off"
+      :
+      : "v"(src), "s"(lds)
+      : "memory");
+}
+
 template <int QT, bool F8, int DP, int CT>
-__global__ void __launch_bounds__(kThreads, CT == 1 && DP <= 128 ? 2 : 1)
-    dresd_attend_wave(AttendPlan pl) {
+__global__ void __launch_bounds__(kThreads, (Ring<F8, DP>::kPair ? 2 : 1)) dresd_attend_wave(AttendPlan pl) {
   typedef Half<QT> H;
   typedef typename H::v8 v8;
-  constexpr int KT = tile_keys(F8), U = KT / 32;  // 32-key groups of a tile
+  typedef Ring<F8, DP> R;
+  constexpr int KT = R::kKeys, U = KT / 16;       // 16-key groups of a tile
   constexpr int KS = DP / 32;                     // 32-dim steps
-  constexpr int VR = F8 ? DP / 32 : DP / 16;      // value loads per 32 keys
-  constexpr int VL = F8 ? DP / 16 : DP / 8;       // lanes of a value row
+  constexpr int NS = R::kSlots;
   extern __shared__ __align__(16) uint8_t lds[];
-  const int tid = threadIdx.x, lane = tid & 63, wid = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, kq = lane >> 4;
   Unit u;
   if (!unit_of(pl, u)) return;
   const AttendParams &p = pl.p;
   const int D = p.c.dim;
 
-  uint8_t *vt = lds + (size_t)wid * wave_bytes(F8, DP);
-  int64_t *offs = reinterpret_cast<int64_t *>(vt + (size_t)KT * DP * 2);
-  float *kf = reinterpret_cast<float *>(offs + KT), *vf = kf + KT;
+  uint8_t *ring = lds + (size_t)wid * R::kBytes;
+  int64_t *offs = reinterpret_cast<int64_t *>(ring + NS * 2 * R::kHalf);
+  const int32_t *ids = reinterpret_cast<const int32_t *>(offs + KT);
+  const uint32_t *exps = reinterpret_cast<const uint32_t *>(ids + 2 * NS * KT);
+  const uint32_t ring_at = lds_address(ring);
+  const uint32_t ids_at = ring_at + NS * 2 * R::kHalf + R::kOffs, exps_at = ids_at + R::kIds;
 
   // queries: operand of row 16 c + col, dims in the order in which keys are read
   v8 q[CT][KS];
@@ -101,7 +149,7 @@ __global__ void __launch_bounds__(kThreads, CT == 1 && DP <= 128 ? 2 : 1)
     for (int d = 0; d < DP / 16; ++d) acc[c][d] = f4{0.f, 0.f, 0.f, 0.f};
   }
 
-  // this split's tiles
+  // this split's tiles; tile i of this wave is t0 + kWaves i, i < count
   const int end = reach(pl, u, pl.rows);
   const int tiles = end > 0 ? (end + KT - 1) / KT : 0;
   // (whole rounds of the four waves)
@@ -109,201 +157,234 @@ __global__ void __launch_bounds__(kThreads, CT == 1 && DP <= 128 ? 2 : 1)
   const int64_t lo = (int64_t)u.split * per;
   const int first = lo < tiles ? (int)lo : tiles;
   const int last = first + per < tiles ? first + per : tiles;
+  const int t0 = first + wid;
+  const int count = t0 < last ? (last - t0 + kWaves - 1) / kWaves : 0;
 
+  const int row_bytes = F8 ? D : 2 * D;
+  const int in_page = (1 << p.c.page_log) - 1;
+  const int32_t *table = p.table + (int64_t)u.b * p.width;
+  // rows of this cache head: page * page_rows + position in the page
+  const int64_t page_rows = (int64_t)p.c.heads << p.c.page_log;
+  const int64_t head_row = (int64_t)u.head << p.c.page_log;
   const uint8_t *kbase = static_cast<const uint8_t *>(p.c.k);
   const uint8_t *vbase = static_cast<const uint8_t *>(p.c.v);
-  const int row_bytes = F8 ? D : 2 * D;
-  const int32_t *table = p.table + (int64_t)u.b * p.width;
-  const int in_page = (1 << p.c.page_log) - 1;
 
-  // page of this lane's key of a tile (lanes past the tile: unused)
-  auto page_of = [&](int t) -> int {
-    if (t >= last || lane >= KT) return -1;
-    const int pos = t * KT + lane;
-    return pos < u.L ? table[pos >> p.c.page_log] : -1;
+  // chunk exchange of a row of keys and of values (16-byte chunks: exclusive or)
+  auto kswap = [](int k) -> int {
+    if constexpr (F8) return DP == 64 ? (k >> 2) & 3 : DP == 128 ? (k >> 1) & 7 : k & 15;
+    else return DP == 64 ? (k >> 1) & 7 : k & 15;
   };
-  // offsets of a tile's rows into LDS; which of its keys there are
-  uint32_t ke = 0, ve = 0;                        // their exponents
-  auto place = [&](int t, int page) -> uint64_t {
-    const bool ok = (uint32_t)page < (uint32_t)p.c.pages;
-    const int64_t r = ok ? ((((int64_t)page * p.c.heads + u.head) << p.c.page_log) +
-                            ((t * KT + lane) & in_page))
-                         : 0;
-    if (lane < KT) offs[lane] = r * row_bytes;
-    if constexpr (F8) {
-      ke = ok ? p.c.k_exp[r] : 127u;
-      ve = ok ? p.c.v_exp[r] : 127u;
-    }
-    return __ballot(ok);
+  auto vswap = [&](int k) -> int {
+    if constexpr (F8) return kswap(k);
+    else return (DP == 64 ? (k >> 1) & 3 : k & 7) << 1;
   };
-
-  u4 kr[U][2][F8 ? KS / 2 : KS], vr[U][VR];
-  const int vl = lane % VL, vk = lane / VL;       // 16 bytes of a row, row within a load
-  // Where the head is narrower than DP, the dims past it are read from the row's
-  // start: against queries of zero, and for outputs that are not stored.
-  int kd[F8 ? KS / 2 : KS];
+  // what this lane copies of a row: keys' and values' bytes.  Where the head is narrower
+  // than DP, the dims past it are its first ones again: against queries of zero, and
+  // for outputs that are not stored.
+  constexpr int kPer = R::kPitch / 16;            // lanes of a row
+  const int crow = lane / kPer;
+  int kat[R::kCopies], vat[R::kCopies];
 #pragma unroll
-  for (int i = 0; i < (F8 ? KS / 2 : KS); ++i) {
-    const int d = F8 ? 64 * i + 16 * kq : 32 * i + 8 * kq;
-    kd[i] = d < D ? (F8 ? d : 2 * d) : 0;
+  for (int j = 0; j < R::kCopies; ++j) {
+    const int k = R::kRows * j + crow, c = lane % kPer;
+    kat[j] = 16 * (c ^ kswap(k));
+    vat[j] = 16 * (c ^ vswap(k));
+    kat[j] = kat[j] < row_bytes ? kat[j] : 0;
+    vat[j] = vat[j] < row_bytes ? vat[j] : 0;
   }
-  const int vd = 16 * vl < row_bytes ? 16 * vl : 0;
-  // (rows of 8-bit caches are 8-byte aligned, and may end inside 16 bytes, at odd multiples of 8)
-  auto load16 = [&](auto halves, const uint8_t *src, int at) -> u4 {
-    if constexpr (decltype(halves)::value) {
-      const u2 a = *reinterpret_cast<const u2 *>(src + at);
-      const u2 b = *reinterpret_cast<const u2 *>(src + (at + 8 < row_bytes ? at + 8 : at));
-      return u4{a[0], a[1], b[0], b[1]};
-    } else {
-      return *reinterpret_cast<const u4 *>(src + at);
+
+  // page ids of tile i (one operation; nothing for positions past the last)
+  auto fetch_ids = [&](int i) {
+    const int pos = (t0 + kWaves * i) * KT + lane;
+    if (lane < KT && pos < u.L)
+      copy1_to_lds(table + (pos >> p.c.page_log), ids_at + (i % (2 * NS)) * KT * 4);
+  };
+  // page id of this lane's key of tile i, -1 where there is none
+  const int klane = lane & (KT - 1);
+  auto page_of = [&](int i) -> int {
+    const int pos = (t0 + kWaves * i) * KT + klane, id = ids[(i % (2 * NS)) * KT + klane];
+    return pos < u.L && (uint32_t)id < (uint32_t)p.c.pages ? id : -1;
+  };
+  // row of this lane's key of tile i (of the first page, where there is none); the offsets of
+  // the tile's rows go to LDS
+  auto place = [&](int i, int page) -> int64_t {
+    const int64_t r = (int64_t)(page < 0 ? 0 : page) * page_rows + head_row +
+                      (((t0 + kWaves * i) * KT + klane) & in_page);
+    offs[klane] = r * row_bytes;
+    return r;
+  };
+  // keys and values of tile i, of row r for this lane's key (kOps operations)
+  auto fetch = [&](int i, int64_t r) {
+    const uint32_t at = ring_at + (i % NS) * 2 * R::kHalf;
+    int64_t o[R::kCopies];
+#pragma unroll
+    for (int j = 0; j < R::kCopies; ++j) o[j] = offs[R::kRows * j + crow];
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the slot has been read
+    if constexpr (F8) {
+      const uint32_t e = exps_at + (i % NS) * KT * 8;
+      if (lane < KT) {
+        copy_byte_from(p.c.k_exp + r, e);
+        copy_byte_from(p.c.v_exp + r, e + KT * 4);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < R::kCopies; ++j) {
+      copy16_from(kbase + o[j] + kat[j], at + 1024 * j);
+      copy16_from(vbase + o[j] + vat[j], at + R::kHalf + 1024 * j);
     }
   };
-  auto load_tile = [&](auto halves) {
-#pragma unroll
-    for (int g = 0; g < U; ++g)
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const uint8_t *src = kbase + offs[32 * g + 16 * s + col];
-#pragma unroll
-        for (int i = 0; i < (F8 ? KS / 2 : KS); ++i) kr[g][s][i] = load16(halves, src, kd[i]);
-      }
-#pragma unroll
-    for (int g = 0; g < U; ++g)
-#pragma unroll
-      for (int i = 0; i < VR; ++i)
-        vr[g][i] = load16(halves, vbase + offs[32 * g + (64 / VL) * i + vk], vd);
-  };
-  auto load = [&]() {
-    if (F8 && (D & 8)) load_tile(std::true_type{});
-    else load_tile(std::false_type{});
-  };
-  // LDS address of 16-byte chunk c of key k: the 32-byte pairs of 8 keys that are
-  // read together lie in different banks
-  auto chunk = [&](int k, int c) -> uint8_t * {
-    return vt + ((size_t)k * (DP / 8) + (c ^ ((DP == 64 ? (k >> 1) & 3 : k & 7) << 1))) * 16;
-  };
 
-  // one tile: its keys and values are in registers, ok its keys that there are
-  auto compute = [&](int t, bool masked, uint64_t ok, int next, int next_page,
-                     uint64_t &next_ok) {
+  const int plain = seen_by_all(pl, u);
+  if (count > 0) {
+    const int ahead = count < 2 * NS ? count : 2 * NS;
+    for (int i = 0; i < ahead; ++i) fetch_ids(i);
+    wait_vmcnt<0>();
+    const int begin = count < NS ? count : NS;
+    for (int i = 0; i < begin; ++i) {
+      const int64_t r = place(i, page_of(i));
+      wave_sync_lds();
+      fetch(i, r);
+    }
+  }
+  for (int i = 0; i < count; ++i) {
+    // Tile i is here when no more operations are under way than the tiles after it
+    // have (page ids among them only make the wait longer).
+    if (i + NS - 1 < count) wait_vmcnt<(NS - 1) * R::kOps>();
+    else wait_vmcnt<0>();
+    const int t = t0 + kWaves * i;
+    uint8_t *kt = ring + (i % NS) * 2 * R::kHalf, *vt = kt + R::kHalf;
+
+    // Everything of the tile that is read from LDS is on its way before the first product:
+    // keys, values (transposed), exponents, page ids of this tile and of the next in its slot.
+    u4 kx[U][F8 ? KS / 2 : KS];
+#pragma unroll
+    for (int g = 0; g < U; ++g) {
+      const int k = 16 * g + col;
+#pragma unroll
+      for (int n = 0; n < (F8 ? KS / 2 : KS); ++n)
+        kx[g][n] = *reinterpret_cast<const u4 *>(kt + k * R::kPitch +
+                                                 16 * ((4 * n + kq) ^ kswap(k)));
+    }
+    const int page = page_of(i), next = i + NS < count ? i + NS : i;
+    const int next_page = page_of(next);
+    const uint32_t *ke = exps + (i % NS) * KT * 2, *ve = ke + KT;
+    u4 kb[U], vb[U];
+    if constexpr (F8)
+#pragma unroll
+      for (int g = 0; g < U; ++g) {
+        kb[g] = *reinterpret_cast<const u4 *>(ke + 16 * g + 4 * kq);
+        vb[g] = *reinterpret_cast<const u4 *>(ve + 16 * g + 4 * kq);
+      }
+    u2 vx[DP / 16];
+    auto read_values = [&]() {
+      // 16 bit: rows 4 kq .. + 3; 8 bit: of either group, the 8 keys of this lane's weights
+      const int r = F8 ? col >> 1 : col >> 2, k = F8 ? 4 * kq + (r & 3) + 16 * (r >> 2) : 4 * kq + r;
+      const uint8_t *vr = vt + k * R::kPitch + 8 * (col & 1);
+#pragma unroll
+      for (int d = 0; d < DP / 16; ++d) {
+        if constexpr (F8) vx[d] = read_transposed8(vr + 16 * (d ^ vswap(k)));
+        else
+          vx[d] = __builtin_bit_cast(
+              u2, read_transposed(vr + 16 * ((2 * d + ((col & 3) >> 1)) ^ vswap(k))));
+      }
+    };
+    read_values();
+
     // scores, rows of keys x columns of query rows
-    f4 s[CT][U][2];
+    f4 s[CT][U];
 #pragma unroll
     for (int g = 0; g < U; ++g)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int c = 0; c < CT; ++c) s[c][g] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int c = 0; c < CT; ++c) s[c][g][h] = f4{0.f, 0.f, 0.f, 0.f};
+    for (int n = 0; n < (F8 ? KS / 2 : KS); ++n)
 #pragma unroll
-        for (int i = 0; i < KS; ++i) {
-          v8 k;
-          if constexpr (F8) {
-            const u4 x = kr[g][h][i / 2];
-            k = from_f8<QT>(i & 1 ? u2{x[2], x[3]} : u2{x[0], x[1]});
-          } else {
-            k = __builtin_bit_cast(v8, kr[g][h][i]);
-          }
+      for (int g = 0; g < U; ++g) {
+        const u4 x = kx[g][n];
+        if constexpr (F8) {
+          const v8 a = from_f8<QT>(u2{x[0], x[1]}), b = from_f8<QT>(u2{x[2], x[3]});
 #pragma unroll
-          for (int c = 0; c < CT; ++c) s[c][g][h] = H::mfma16(k, q[c][i], s[c][g][h]);
+          for (int c = 0; c < CT; ++c) s[c][g] = H::mfma16(a, q[c][2 * n], s[c][g]);
+#pragma unroll
+          for (int c = 0; c < CT; ++c) s[c][g] = H::mfma16(b, q[c][2 * n + 1], s[c][g]);
+        } else {
+          const v8 a = __builtin_bit_cast(v8, x);
+#pragma unroll
+          for (int c = 0; c < CT; ++c) s[c][g] = H::mfma16(a, q[c][n], s[c][g]);
         }
       }
-    // values into LDS; where not every row sees all keys, keys that are not there as zeros,
-    // and keys with a value that is not finite apart
+    const int64_t next_row = place(next, next_page);
+    const uint64_t there = __ballot(page >= 0 && lane < KT), whole = (1ull << KT) - 1;
+    const bool masked = (t + 1) * KT > plain || there != whole;
+
+    // Where not every row sees all keys, keys that are not there become zeros, and
+    // keys with a value that is not finite are kept apart, for the rows that do not see them.
     uint64_t bad = 0;
     if (masked) {
-      if constexpr (F8) bad = __ballot(lane < KT && ve == 255u);
-#pragma unroll
-      for (int g = 0; g < U; ++g)
-#pragma unroll
-        for (int i = 0; i < VR; ++i) {
-          constexpr int RL = 64 / VL;             // rows of a load
-          if (!(((ok >> vk) >> (32 * g + RL * i)) & 1)) vr[g][i] = u4{};
-          uint64_t w = __ballot(drop_nonfinite<QT, F8>(vr[g][i]));
-          while (w) {                             // rare
-            const int j = __ffsll((long long)w) - 1;
-            bad |= 1ull << (32 * g + RL * i + j / VL);
-            w &= w - 1;
-          }
-        }
-    }
-    if constexpr (F8) {
-      if (lane < KT) {
-        kf[lane] = __uint_as_float(ke << 23);
-        vf[lane] = value_factor(ve, masked);
-      }
-    }
-#pragma unroll
-    for (int g = 0; g < U; ++g)
-#pragma unroll
-      for (int i = 0; i < VR; ++i) {
-        const int k = 32 * g + (64 / VL) * i + vk;
-        if constexpr (F8) {
-          *reinterpret_cast<v8 *>(chunk(k, 2 * vl)) = from_f8<QT>(u2{vr[g][i][0], vr[g][i][1]});
-          *reinterpret_cast<v8 *>(chunk(k, 2 * vl + 1)) = from_f8<QT>(u2{vr[g][i][2], vr[g][i][3]});
-        } else {
-          *reinterpret_cast<u4 *>(chunk(k, vl)) = vr[g][i];
+      if constexpr (F8) bad = __ballot(lane < KT && ve[klane] == 255u);
+      for (int j = 0; j < R::kCopies; ++j) {
+        u4 *at = reinterpret_cast<u4 *>(vt + 1024 * j + 16 * lane);
+        u4 x = *at;
+        if (!((there >> (R::kRows * j + crow)) & 1)) x = u4{};
+        uint64_t w = __ballot(drop_nonfinite<QT, F8>(x));
+        *at = x;
+        while (w) {                               // rare
+          const int n = __ffsll((long long)w) - 1;
+          bad |= 1ull << (R::kRows * j + n / kPer);
+          w &= w - 1;
         }
       }
-    wave_sync_lds();
-    f4 kfac[U][2], vfac[U][2];
-    if constexpr (F8) {
-#pragma unroll
-      for (int g = 0; g < U; ++g)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          kfac[g][h] = *reinterpret_cast<const f4 *>(kf + 32 * g + 16 * h + 4 * kq);
-          vfac[g][h] = *reinterpret_cast<const f4 *>(vf + 32 * g + 16 * h + 4 * kq);
-        }
-    }
-    // the next tile is on its way while this one's weights are formed
-    wave_sync_lds();
-    if (next < last) {
-      next_ok = place(next, next_page);
       wave_sync_lds();
-      load();
-    }
-    // weights
-    v8 w[CT][U];
-#pragma unroll
-    for (int c = 0; c < CT; ++c) {
+      read_values();
+      // (byte 255 is no factor: rows that do not see the key are to have nothing of it)
       if constexpr (F8)
 #pragma unroll
         for (int g = 0; g < U; ++g)
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
+          for (int e = 0; e < 4; ++e) vb[g][e] = vb[g][e] == 255u ? 0u : vb[g][e];
+    }
+
+    // weights
+    f4 vfac[U];
+    if constexpr (F8) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[c][g][h][i] *= kfac[g][h][i];
-      if (masked) {
-        const uint64_t see = (window(pl, u, row[c], tok[c], t * KT) & ok) >> (4 * kq);
-        const uint64_t inf = bad >> (4 * kq);
+      for (int g = 0; g < U; ++g) {
 #pragma unroll
-        for (int g = 0; g < U; ++g) {
-          const uint32_t is = (uint32_t)(see >> (32 * g)), no = (uint32_t)(inf >> (32 * g));
+        for (int e = 0; e < 4; ++e) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float x = s[c][g][h][i];
-              x = (no >> (16 * h + i)) & 1 ? __builtin_nanf("") : x;
-              s[c][g][h][i] = (is >> (16 * h + i)) & 1 ? x : -__builtin_huge_valf();
-            }
+          for (int c = 0; c < CT; ++c) s[c][g][e] *= __uint_as_float(kb[g][e] << 23);
+          vfac[g][e] = __uint_as_float(vb[g][e] << 23);
         }
+      }
+    }
+    u2 w[CT][U];
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+      if (masked) {
+        const uint64_t see = (window(pl, u, row[c], tok[c], t * KT) & there) >> (4 * kq);
+        const uint32_t is = (uint32_t)see, no = (uint32_t)(bad >> (4 * kq));
+#pragma unroll
+        for (int g = 0; g < U; ++g)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float x = s[c][g][e];
+            x = (no >> (16 * g + e)) & 1 ? __builtin_nanf("") : x;
+            s[c][g][e] = (is >> (16 * g + e)) & 1 ? x : -__builtin_huge_valf();
+          }
       }
       float top = -3e38f;
 #pragma unroll
       for (int g = 0; g < U; ++g)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float x = s[c][g][h][i];
-            if constexpr (F8 && QT == kF16) {
-              // the largest weight is that of the value as it is stored
-              const int e = (int)((__float_as_uint(vfac[g][h][i]) >> 23) & 255u) - 127;
-              x = x * c2 + (float)(e < -60 ? -60 : e > 20 ? 20 : e);
-            }
-            top = fmaxf(top, x);
+        for (int e = 0; e < 4; ++e) {
+          float x = s[c][g][e];
+          if constexpr (F8 && QT == kF16) {
+            // the largest weight is that of the value as it is stored
+            const int ex = (int)((__float_as_uint(vfac[g][e]) >> 23) & 255u) - 127;
+            x = x * c2 + (float)(ex < -60 ? -60 : ex > 20 ? 20 : ex);
           }
+          top = fmaxf(top, x);
+        }
       if constexpr (!(F8 && QT == kF16)) top *= c2;  // (in powers of two)
       if (__any(top > m[c] + H::kSlack)) {
         top = fmaxf(top, __shfl_xor(top, 16, kWaveSize));
@@ -315,92 +396,77 @@ __global__ void __launch_bounds__(kThreads, CT == 1 && DP <= 128 ? 2 : 1)
 #pragma unroll
         for (int d = 0; d < DP / 16; ++d)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) acc[c][d][i] *= a;
+          for (int e = 0; e < 4; ++e) acc[c][d][e] *= a;
       }
       const float ref = m[c] - H::kBias;
       float sum = 0.f;
 #pragma unroll
-      for (int g = 0; g < U; ++g)
+      for (int g = 0; g < U; ++g) {
+        uint16_t r[4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float x = exp2_hw(fmaf(s[c][g][h][i], c2, -ref));
-            sum += x;
-            if constexpr (F8) x *= vfac[g][h][i];
-            w[c][g][4 * h + i] = H::round(x);
-          }
+        for (int e = 0; e < 4; ++e) {
+          float x = exp2_hw(fmaf(s[c][g][e], c2, -ref));
+          sum += x;
+          if constexpr (F8) x *= vfac[g][e];
+          r[e] = __builtin_bit_cast(uint16_t, H::round(x));
+        }
+        w[c][g] = u2{r[0] | (uint32_t)r[1] << 16, r[2] | (uint32_t)r[3] << 16};
+      }
       l[c] += sum;
     }
+
     // O^T += V^T P^T
 #pragma unroll
-    for (int g = 0; g < U; ++g)
+    for (int d = 0; d < DP / 16; ++d) {
+      if constexpr (F8) {
+        const v8 x = from_f8<QT>(vx[d]);
 #pragma unroll
-      for (int d = 0; d < DP / 16; ++d) {
-        const int k = 32 * g + 4 * kq + (col >> 2);
-        const int at = 2 * d + ((col & 3) >> 1), in = (col & 1) * 8;
-        const s4v a = read_transposed(chunk(k, at) + in);
-        const s4v b = read_transposed(chunk(k + 16, at) + in);
-        typedef short s8v __attribute__((ext_vector_type(8)));
-        const v8 x = __builtin_bit_cast(
-            v8, s8v{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
+        for (int c = 0; c < CT; ++c)
+          acc[c][d] = H::mfma16(
+              x, __builtin_bit_cast(v8, u4{w[c][0][0], w[c][0][1], w[c][1][0], w[c][1][1]}),
+              acc[c][d]);
+      } else {
 #pragma unroll
-        for (int c = 0; c < CT; ++c) acc[c][d] = H::mfma16(x, w[c][g], acc[c][d]);
+        for (int c = 0; c < CT; ++c) acc[c][d] = H::mfma16_half(vx[d], w[c][0], acc[c][d]);
       }
-    wave_sync_lds();
-  };
-
-  int t = first + wid;
-  if (t < last) {
-    uint64_t ok = place(t, page_of(t));
-    wave_sync_lds();
-    load();
-    int page = page_of(t + kWaves);
-    const uint64_t whole = KT == 64 ? ~0ull : (1ull << KT) - 1;
-    const int plain = seen_by_all(pl, u);
-    for (; t < last; t += kWaves) {
-      const int ahead = page_of(t + 2 * kWaves);
-      uint64_t next_ok = 0;
-      // keys that are all there and that every row sees
-      const bool masked = (t + 1) * KT > plain || (ok & whole) != whole;
-      compute(t, masked, ok, t + kWaves, page, next_ok);
-      ok = next_ok;
-      page = ahead;
     }
+    // the slot is free
+    if (i + 2 * NS < count) fetch_ids(i + 2 * NS);
+    if (i + NS < count) fetch(i + NS, next_row);
   }
 
   // the four waves' sums: rows of a wave [16 CT][DP + 4], statistics
-  constexpr int R = 16 * CT, OS = DP + 4;
-  float *o = reinterpret_cast<float *>(lds), *ml = o + (size_t)kWaves * R * OS;
+  constexpr int RW = 16 * CT, OS = DP + 4;
+  float *o = reinterpret_cast<float *>(lds), *ml = o + (size_t)kWaves * RW * OS;
   __syncthreads();
 #pragma unroll
   for (int c = 0; c < CT; ++c) {
     l[c] += __shfl_xor(l[c], 16, kWaveSize);
     l[c] += __shfl_xor(l[c], 32, kWaveSize);
     if (kq == 0) {
-      ml[(wid * R + 16 * c + col) * 2] = m[c];
-      ml[(wid * R + 16 * c + col) * 2 + 1] = l[c];
+      ml[(wid * RW + 16 * c + col) * 2] = m[c];
+      ml[(wid * RW + 16 * c + col) * 2 + 1] = l[c];
     }
 #pragma unroll
     for (int d = 0; d < DP / 16; ++d)
-      *reinterpret_cast<f4 *>(o + (size_t)(wid * R + 16 * c + col) * OS + 16 * d + 4 * kq) =
+      *reinterpret_cast<f4 *>(o + (size_t)(wid * RW + 16 * c + col) * OS + 16 * d + 4 * kq) =
           acc[c][d];
   }
   __syncthreads();
-  for (int e = tid; e < R * (DP / 4); e += kThreads) {
+  for (int e = tid; e < RW * (DP / 4); e += kThreads) {
     const int r = e / (DP / 4), d = (e - r * (DP / 4)) * 4;
     if (u.row0 + r >= u.rows || d >= D) continue;
     float top = -3e38f, sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[(w * R + r) * 2]);
+    for (int n = 0; n < kWaves; ++n) top = fmaxf(top, ml[(n * RW + r) * 2]);
     f4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float a = exp2_hw(ml[(w * R + r) * 2] - top);
-      sum += ml[(w * R + r) * 2 + 1] * a;
-      const f4 y = *reinterpret_cast<const f4 *>(o + (size_t)(w * R + r) * OS + d);
+    for (int n = 0; n < kWaves; ++n) {
+      const float a = exp2_hw(ml[(n * RW + r) * 2] - top);
+      sum += ml[(n * RW + r) * 2 + 1] * a;
+      const f4 y = *reinterpret_cast<const f4 *>(o + (size_t)(n * RW + r) * OS + d);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] += y[i] * a;
+      for (int k = 0; k < 4; ++k) x[k] += y[k] * a;
     }
     const int tk = (u.row0 + r) / pl.group;
     const int64_t out =
@@ -412,11 +478,7 @@ __global__ void __launch_bounds__(kThreads, CT == 1 && DP <= 128 ? 2 : 1)
 template <int QT, bool F8>
 AttendKernel pick(int ct) {
   constexpr int DP = DRESD_ATTEND_DP;
-  if (ct == 1) return dresd_attend_wave<QT, F8, DP, 1>;
-  if (ct == 2) return dresd_attend_wave<QT, F8, DP, 2>;
-  if constexpr (DP <= 128)
-    if (ct == 4) return dresd_attend_wave<QT, F8, DP, 4>;
-  return nullptr;
+  return ct == 1 ? dresd_attend_wave<QT, F8, DP, 1> : dresd_attend_wave<QT, F8, DP, 2>;
 }
 
 }  // namespace
@@ -428,11 +490,11 @@ AttendKernel DRESD_CAT(attend_wave_kernel_, DRESD_ATTEND_DP)(int qt, bool f8, in
   return f8 ? pick<kBF16, true>(ct) : pick<kBF16, false>(ct);
 }
 
-#if DRESD_ATTEND_DP == 128
-size_t attend_wave_lds(bool f8, int dp, int ct) {
-  const size_t a = kWaves * wave_bytes(f8, dp), b = end_bytes(dp, ct);
+size_t DRESD_CAT(attend_wave_lds_, DRESD_ATTEND_DP)(bool f8, int ct) {
+  const size_t a = (size_t)kWaves * (f8 ? Ring<true, DRESD_ATTEND_DP>::kBytes
+                                        : Ring<false, DRESD_ATTEND_DP>::kBytes);
+  const size_t b = end_bytes(DRESD_ATTEND_DP, ct);
   return a > b ? a : b;
 }
-#endif
 
 }  // namespace dresd
