@@ -115,6 +115,38 @@ __device__ __forceinline__ u2 read_transposed8(const uint8_t *lds) {
                                     (__attribute__((address_space(3))) i2 *)(lds)));
 }
 
+typedef __attribute__((address_space(3))) uint8_t lds_byte;
+__device__ __forceinline__ uint32_t lds_address(const uint8_t *p) {
+  return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_byte *)(p));
+}
+// Copies from each lane's own address to LDS: 16 bytes to lds + 16 lane; one byte,
+// widened to a dword, to lds + 4 lane.  copy16_past does not keep what it reads in the caches.
+// Callers wait with wait_vmcnt.
+__device__ __forceinline__ void copy16_from(const uint8_t *src, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %1\n\t"
+      "global_load_lds_dwordx4 %0, off"
+      :
+      : "v"(src), "s"(lds)
+      : "memory");
+}
+__device__ __forceinline__ void copy16_past(const uint8_t *src, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %1\n\t"
+      "global_load_lds_dwordx4 %0, off nt"
+      :
+      : "v"(src), "s"(lds)
+      : "memory");
+}
+__device__ __forceinline__ void copy_byte_from(const uint8_t *src, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %1\n\t"
+      "global_load_lds_ubyte %0, off"
+      :
+      : "v"(src), "s"(lds)
+      : "memory");
+}
+
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Zeros in place of infinities and NaN among 16 bytes of a cache row; whether there

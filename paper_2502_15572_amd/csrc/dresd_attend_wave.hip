@@ -67,29 +67,6 @@ constexpr size_t end_bytes(int dp, int ct) {
   return (size_t)kWaves * 16 * ct * (dp + 4 + 2) * 4;
 }
 
-typedef __attribute__((address_space(3))) uint8_t lds_byte;
-__device__ __forceinline__ uint32_t lds_address(const uint8_t *p) {
-  return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_byte *)(p));
-}
-// Copies from each lane's own address to LDS: 16 bytes to lds + 16 lane; one byte,
-// widened to a dword, to lds + 4 lane.  Callers wait with wait_vmcnt.
-__device__ __forceinline__ void copy16_from(const uint8_t *src, uint32_t lds) {
-  asm volatile(
-      "s_mov_b32 m0, %1\n\t"
-      "global_load_lds_dwordx4 %0, off nt"
-      :
-      : "v"(src), "s"(lds)
-      : "memory");
-}
-__device__ __forceinline__ void copy_byte_from(const uint8_t *src, uint32_t lds) {
-  asm volatile(
-      "s_mov_b32 m0, %1\n\t"
-      "global_load_lds_ubyte %0, off"
-      :
-      : "v"(src), "s"(lds)
-      : "memory");
-}
-
 template <int QT, bool F8, int DP, int CT>
 __global__ void __launch_bounds__(kThreads, (Ring<F8, DP>::kPair ? 2 : 1)) dresd_attend_wave(AttendPlan pl) {
   typedef Half<QT> H;
@@ -229,8 +206,8 @@ __global__ void __launch_bounds__(kThreads, (Ring<F8, DP>::kPair ? 2 : 1)) dresd
     }
 #pragma unroll
     for (int j = 0; j < R::kCopies; ++j) {
-      copy16_from(kbase + o[j] + kat[j], at + 1024 * j);
-      copy16_from(vbase + o[j] + vat[j], at + R::kHalf + 1024 * j);
+      copy16_past(kbase + o[j] + kat[j], at + 1024 * j);
+      copy16_past(vbase + o[j] + vat[j], at + R::kHalf + 1024 * j);
     }
   };
 
