@@ -246,7 +246,9 @@ def time_pipeline(args):
     B hidden states of D fp32 dims -> transform (Eq. 1, a D x d projection
     standing in for the PCA basis, Eq. 2) -> next-token-filtered search of
     the workload's datastore (exact, or partitioned with --ivf P) -> draft
-    assembly into 10 EOS-padded drafts.  Times the whole step."""
+    assembly into 10 EOS-padded drafts.  Times the whole step.  With --verify
+    CTX the step goes on to what batch verification (Section 3.6) does around a
+    model's weights (see verify_step)."""
     import torch
     from datagen import WORKLOADS, generate
     from paper_2502_15572_amd import (Index, PartitionedIndex, kmeans_assign, pack_drafts,
@@ -294,10 +296,14 @@ def time_pipeline(args):
     dout = (torch.empty((B, r, w.L), dtype=torch.int32, device=dev),
             torch.empty((B,), dtype=torch.int32, device=dev))
 
+    verify = verify_step(B, r, w.L, args.verify, dev) if args.verify else None
+
     def step(i):
         transform(xs[i % 64], mean, var, W, out=y)
         search(y, nt, out)
         pack_drafts(out[2], r, w.L, out=dout)
+        if verify:
+            verify(dout[0], dout[1], nt)
 
     for i in range(args.warmup):
         step(i)
@@ -312,9 +318,46 @@ def time_pipeline(args):
         "workload": w.name, "N": w.N, "d": w.d, "D": D, "B": B, "k": k, "drafts": r,
         "search": kind,
         "steps_per_s": args.steps / el, "queries_per_s": args.steps * B / el,
-        "p50_us": p50 * 1e3,
+        "p50_us": p50 * 1e3, "verify_context": args.verify,
         "mean_drafts_kept": float(dout[1].float().mean())}}), flush=True)
     ix.close()
+
+
+def verify_step(B, r, L, ctx, dev):
+    """What one verifying forward does around a model's weights, for one layer
+    of 32 heads of 128 dims over ctx cached tokens a sequence (bf16, pages of
+    16) and 32,000 tokens of vocabulary: the drafts' prefix tree, its keys and
+    values into the cache, its attention, the acceptance of a path, and its
+    entries to their final slots.  Queries, keys, values and logits are random.
+    Returns the call, of (drafts, count, next_tok)."""
+    import torch
+    from paper_2502_15572_amd import accept_drafts, draft_tree, kv_read, kv_write, paged_attention
+    H, D, page, V = 32, 128, 16, 32000
+    N = min(1024, 1 + r * (L - 1))
+    width = -(-(ctx + N) // page)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    kp = torch.randn(B * width, H, page, D, device=dev, generator=gen).to(torch.bfloat16)
+    vp = torch.randn(B * width, H, page, D, device=dev, generator=gen).to(torch.bfloat16)
+    table = torch.randperm(B * width, device=dev, generator=gen).view(B, width).to(torch.int32)
+    qkv = torch.randn(B, N, 3 * H, D, device=dev, generator=gen).to(torch.bfloat16)
+    q, k, v = qkv[:, :, :H], qkv[:, :, H:2 * H].flatten(0, 1), qkv[:, :, 2 * H:].flatten(0, 1)
+    logits = torch.randn(B, N, V, device=dev, generator=gen)
+    lens = torch.full((B,), ctx + N, dtype=torch.int32, device=dev)
+    pos = torch.arange(ctx, ctx + N, device=dev)
+    slots = (table[:, pos // page].long() * page + pos % page).contiguous()
+    flat = slots.flatten()
+    none = torch.full((B, 1), -1, dtype=torch.int64, device=dev)
+
+    def call(drafts, count, next_tok):
+        token, parent, _, mask, nodes = draft_tree(drafts, count, next_tok, N)
+        kv_write(k, v, flat, kp, vp)
+        paged_attention(q, kp, vp, table, lens, mask=mask)
+        path, _, _ = accept_drafts(logits, token, parent, nodes, L)
+        src = torch.cat([slots, none], 1).gather(1, torch.where(path < 0, N, path).long())
+        dst = torch.where(path < 0, none, slots[:, :L])
+        kv_write(*kv_read(src.flatten(), kp, vp), dst.flatten(), kp, vp)
+
+    return call
 
 
 def time_partitioned(args):
@@ -585,6 +628,9 @@ def main():
                     help="only time one decode step of retrieval: B hidden states of D dims -> "
                          "transform -> filtered search (exact, or partitioned with --ivf) -> "
                          "10 drafts")
+    ap.add_argument("--verify", type=int, default=0, metavar="CTX",
+                    help="with --pipeline: the step goes on to one layer of the verifying "
+                         "forward (32 heads of 128) over CTX cached tokens, and acceptance")
     ap.add_argument("--drafts", type=int, default=0, metavar="R",
                     help="only time draft assembly of the workload's k continuations into R "
                          "drafts (Section 3.6)")
