@@ -352,7 +352,7 @@ dresd_status dresd_pack_drafts(const int32_t *tokens, int32_t B, int32_t k, int3
  *   count     device, [B] int32: drafts per query (rows past them are not read
  *             as drafts; values outside [0, r] count as the nearer bound).
  *   next_tok  device, [B] int32.
- *   B >= 0 (0 is a no-op); 1 <= r <= DRESD_K_MAX; 1 <= length <= 4096;
+ *   0 <= B < 2^22 (0 is a no-op); 1 <= r <= DRESD_K_MAX; 1 <= length <= 4096;
  *   1 <= N <= DRESD_NODES_MAX.  1 + r (length - 1) nodes always suffice.
  *   token     device, [B, N] int32 out: token of each node, eos past the last.
  *   parent    device, [B, N] int32 out: its parent, -1 for node 0 and past the
@@ -378,7 +378,8 @@ dresd_status dresd_draft_tree(const int32_t *drafts, const int32_t *count,
  *   k, v          device, [pages, heads, page_size, dim], 16-byte aligned, element
  *                 type dtype: DRESD_F16, DRESD_BF16 or DRESD_F8.
  *   k_exp, v_exp  DRESD_F8: device, [pages, heads, page_size] uint8: a row's
- *                 values are its stored ones times 2^(exp - 127).  NULL otherwise.
+ *                 values are its stored ones times 2^(exp - 127); 1 <= exp <= 254 (as
+ *                 dresd_kv_write stores it) where a row is read.  NULL otherwise.
  *   1 <= pages < 2^31; page_size a power of two, at most 65536;
  *   1 <= heads <= 65535; dim a multiple of 8 in [8, 256].
  */
@@ -398,7 +399,8 @@ typedef struct {
  *   slots     device, [n] int64: each token's slot.  A token whose slot is outside
  *             [0, pages * page_size) (-1, say) is skipped.  Two tokens of one call
  *             must not share a slot (not checked: its contents would be a mixture).
- *   n >= 0 (0 is a no-op).
+ *   n >= 0 (0 is a no-op), and n heads at most 2^29 - 32 for dim <= 64, 2^28 - 32
+ *   for dim <= 128, else 2^27 - 32.
  * 16-bit caches hold the values rounded to nearest even.  DRESD_F8: a row (one
  * token of one head) is stored at the smallest power of two, not below 2^-126,
  * at which its largest magnitude is at most 448 (a zero row: 2^-9), its
@@ -443,8 +445,10 @@ dresd_status dresd_kv_read(const dresd_kv_cache *cache, const int64_t *slots, in
  *             h / (q_heads / heads).
  *   starts    device, [B + 1] int32: sequence b's chunk is rows starts[b] to
  *             starts[b + 1] - 1, n_b of them, possibly none; rows before
- *             starts[0], from starts[B] on and outside [0, T) are left as they
- *             were.  Or NULL: T = B n, and every chunk has n rows.
+ *             starts[0] and from starts[B] on are left as they were.  They
+ *             ascend within [0, T] (not checked: where they do not, nothing outside
+ *             the T rows is touched, but what they hold is not defined).
+ *             Or NULL: T = B n, and every chunk has n rows.
  *   n         tokens per chunk without starts (ignored with them).
  *   T         rows of q and out, T * q_heads < 2^31; T = 0 is a no-op.
  *   table     device, [B, width] int32, width >= 1, 0 <= B heads <= 2^30: page ids.
@@ -459,11 +463,13 @@ dresd_status dresd_kv_read(const dresd_kv_cache *cache, const int64_t *slots, in
  *             dresd_paged_attention_workspace says for these arguments (which
  *             reads no device memory).  Used by this call alone until `stream`
  *             has completed it; its contents do not matter.
- * What masked positions hold does not matter, infinities and NaN included.
+ * What masked positions hold does not matter, infinities and NaN included; a row that
+ * sees a key or a value that is not finite may become NaN throughout.
  * Scores, softmax statistics and sums are fp32; keys and queries enter the
  * matrix cores unrounded, a row's weights rounded to dtype.  Deterministic.
  * Errors: EINVAL (null pointer with T > 0, ranges, alignment, dtypes that do not
- * fit, too little workspace), EDEVICE.
+ * fit, too little workspace, more than some 2^24 blocks of the 16 to 128 rows of a
+ * cache head that are computed together), EDEVICE.
  */
 dresd_status dresd_paged_attention(const dresd_kv_cache *cache, const void *q, int64_t q_row,
                                    int64_t q_head, int32_t dtype, int32_t q_heads,
@@ -487,7 +493,7 @@ dresd_status dresd_paged_attention_workspace(const dresd_kv_cache *cache, int32_
  *             b starts at (b N + u) * row elements, row >= V.
  *   token, parent  device, [B, N] int32, nodes device, [B] int32: the tree
  *             (dresd_draft_tree; nodes outside [0, N] count as the nearer bound).
- *   B >= 0 (0 is a no-op); 1 <= N <= DRESD_NODES_MAX; 1 <= V < 2^31;
+ *   0 <= B < 2^22 (0 is a no-op); 1 <= N <= DRESD_NODES_MAX; 1 <= V <= 2^30;
  *   1 <= most <= DRESD_NODES_MAX.
  *   path      device, [B, most] int32 out: the accepted nodes, -1 past them.
  *   accepted  device, [B] int32 out: their number, >= 1 (0 for an empty tree).

@@ -568,7 +568,7 @@ def paged_attention(q, k_pages, v_pages, table, lengths, starts=None, mask=None,
     with ``mask`` (int64 [B, n, words] or [T, words]; ``draft_tree``) all before the
     chunk and the chunk tokens whose bit is set.  ``scale`` defaults to dim ** -0.5.
     Returns the output, shaped as q and in its type (zeros for a row that sees
-    nothing; rows outside every chunk are left as they were), and with ``with_lse``
+    nothing; rows outside every chunk are left as they were; no gradient), and with ``with_lse``
     also the fp32 logarithms of the rows' sums ([..., q_heads]; -inf for a row
     that sees nothing).  ``out``: the output tensor, or the pair."""
     import torch

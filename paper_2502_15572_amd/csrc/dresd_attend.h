@@ -248,8 +248,9 @@ __device__ __forceinline__ bool unit_of(const AttendPlan &pl, Unit &u) {
     u.n = __builtin_amdgcn_readfirstlane(u.n);
     u.token0 = __builtin_amdgcn_readfirstlane((int)u.token0);
   }
-  u.row0 = blk * pl.rows;
   u.rows = u.n * pl.group;
+  if (blk < 0 || blk > (u.rows - 1) / pl.rows) return false;  // (chunks that overlap)
+  u.row0 = blk * pl.rows;
   u.len = p.lengths[u.b];
   u.before = (int64_t)u.len - u.n < -0x40000000 ? -0x40000000 : u.len - u.n;
   const int64_t room = (int64_t)p.width << p.c.page_log;

@@ -39,6 +39,7 @@ namespace {
 
 constexpr int kSplitsMax = 64;
 constexpr int kJoinThreads = 256;
+constexpr int64_t kGroupsMax = (1 << 24) - 8;  // workgroups of 256 threads: a launch has fewer than 2^32
 
 // Joins the parts of every row and head: `GS` 32-lane groups of a workgroup a row, of
 // which each takes every GS-th part, four dims a lane (the dims past 128 in a second
@@ -145,6 +146,7 @@ int64_t part_floats(const AttendPlan &pl) {
 
 int64_t attend_workspace(const AttendParams &p, int cus) {
   const AttendPlan pl = plan_of(p, cus);
+  if (pl.total > kGroupsMax) return -1;
   return part_floats(pl) * (p.c.dim + 2) * 4;
 }
 

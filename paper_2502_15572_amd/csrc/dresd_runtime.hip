@@ -1445,7 +1445,7 @@ dresd_status dresd_draft_tree(const int32_t *drafts, const int32_t *count,
                               int32_t eos, int32_t N, int32_t *token, int32_t *parent,
                               int32_t *depth, uint64_t *mask, int32_t *nodes,
                               dresd_stream stream) {
-  if (B < 0) return fail(DRESD_EINVAL, "B must be >= 0");
+  if (B < 0 || B > kQueriesMax) return fail(DRESD_EINVAL, "B out of range");
   if (r < 1 || r > DRESD_K_MAX) return fail(DRESD_EINVAL, "r must be in [1, DRESD_K_MAX]");
   if (length < 1 || length > 4096) return fail(DRESD_EINVAL, "length out of range");
   if (N < 1 || N > DRESD_NODES_MAX) return fail(DRESD_EINVAL, "N must be in [1, DRESD_NODES_MAX]");
@@ -1475,7 +1475,7 @@ dresd_status dresd_accept_drafts(const void *logits, int32_t dtype, int64_t row,
                                  const int32_t *nodes, int32_t B, int32_t N, int32_t most,
                                  int32_t *path, int32_t *accepted, int32_t *next_tok,
                                  dresd_stream stream) {
-  if (B < 0) return fail(DRESD_EINVAL, "B must be >= 0");
+  if (B < 0 || B > kQueriesMax) return fail(DRESD_EINVAL, "B out of range");
   if (dtype < DRESD_F32 || dtype > DRESD_BF16) return fail(DRESD_EINVAL, "unknown dtype");
   if (V < 1 || V > (1 << 30)) return fail(DRESD_EINVAL, "V out of range");
   if (row < V || row > ((int64_t)1 << 40)) return fail(DRESD_EINVAL, "row out of range");
@@ -1548,7 +1548,7 @@ bool stride_ok(int64_t s) { return s >= 0 && s <= kStrideMax; }
 
 dresd_status check_tokens(const CacheRef &c, int64_t n, int32_t dtype) {
   if (dtype < DRESD_F32 || dtype > DRESD_BF16) return fail(DRESD_EINVAL, "unknown dtype");
-  if (n < 0 || n > 0x7fffffffLL / c.heads) return fail(DRESD_EINVAL, "n out of range");
+  if (n < 0 || n > kv_rows_max(c.dim) / c.heads) return fail(DRESD_EINVAL, "n out of range");
   return DRESD_OK;
 }
 
@@ -1643,7 +1643,9 @@ dresd_status dresd_paged_attention_workspace(const dresd_kv_cache *cache, int32_
   dresd_status s = attend_shape(cache, q_heads, ragged != 0, n, B, T, width, &p);
   if (s == DRESD_OK) s = compute_units(&cus);
   if (s != DRESD_OK) return s;
-  *bytes = attend_workspace(p, cus);
+  const int64_t need = attend_workspace(p, cus);
+  if (need < 0) return fail(DRESD_EINVAL, "too many blocks for one call");
+  *bytes = need;
   return DRESD_OK;
 }
 
@@ -1685,6 +1687,7 @@ dresd_status dresd_paged_attention(const dresd_kv_cache *cache, const void *q, i
   p.dtype = dtype;
   if ((s = compute_units(&cus)) != DRESD_OK) return s;
   const int64_t need = attend_workspace(p, cus);
+  if (need < 0) return fail(DRESD_EINVAL, "too many blocks for one call");
   if (need > 0 && (!work || work_bytes < need || (uintptr_t)work % 16))
     return fail(DRESD_EINVAL, "workspace of " + std::to_string(need) + " bytes needed");
   DRESD_HIP(launch_attend(p, cus, static_cast<hipStream_t>(stream)));

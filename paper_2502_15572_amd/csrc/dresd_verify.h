@@ -8,6 +8,13 @@ namespace dresd {
 constexpr int kF8 = 3;               // DRESD_F8: e4m3, caches alone
 constexpr int kNodesMax = 1024;      // DRESD_NODES_MAX
 constexpr int kHeadDimMax = 256;     // widest head of a cache
+// A launch has fewer than 2^32 threads: queries of a call whose workgroups have 1,024, ...
+constexpr int kQueriesMax = (1 << 22) - 1;
+// ... and rows (tokens times heads) of a cache write or read, dim / 8 lanes each, rounded up to
+// 8, 16 or 32.
+constexpr int64_t kv_rows_max(int dim) {
+  return (dim <= 64 ? 1ll << 29 : dim <= 128 ? 1ll << 28 : 1ll << 27) - 32;
+}
 
 // Prefix tree of drafts (dresd_tree.hip).
 struct TreeParams {
@@ -65,6 +72,7 @@ struct AttendParams {
   int dtype, q_heads, n, B, width, words;
   bool ragged;
 };
+// Bytes; -1: more blocks than one launch takes.
 int64_t attend_workspace(const AttendParams &p, int cus);
 hipError_t launch_attend(const AttendParams &p, int cus, hipStream_t st);
 

@@ -356,3 +356,60 @@ def test_streams_and_repeats(gpu_lib):
     outs = [paged_attention(*args, **kw, stream=s) for _ in range(5) for s in streams]
     torch.cuda.synchronize()
     assert all(torch.equal(o, want) for o in outs)
+
+
+@pytest.mark.parametrize("n", [1, 12, 150])
+@pytest.mark.parametrize("dtype,cache", [("f16", "f16"), ("bf16", "f8")])
+def test_shared_pages(gpu_lib, n, dtype, cache):
+    """Sequences with the same first pages, and a page twice in one table, give what copies of the
+    pages give."""
+    from paper_2502_15572_amd import paged_attention
+    say("attend: shared pages", n, dtype, cache)
+    c = Case(5, [640 - n, 640 - n], [n, n], 2, 2, 128, 64, dtype, cache)
+    (q, kp, vp, table, lens), kw = c.tensors()
+    q[1] = q[0]
+    shared = table.clone()
+    shared[1, :8] = shared[0, :8]                          # then pages of its own
+    shared[:, 3] = shared[:, 1]
+    args, ex = [kp.clone(), vp.clone()], {}
+    for x in args:
+        y = x.view(torch.uint8)
+        for b in (0, 1):
+            y[table[b, :10].long()] = y[shared[b, :10].long()].clone()
+    for name in ("k_exp", "v_exp"):
+        ex[name] = kw[name]
+        if kw[name] is not None:
+            ex[name] = kw[name].clone()
+            for b in (0, 1):
+                ex[name][table[b, :10].long()] = kw[name][shared[b, :10].long()].clone()
+    got = paged_attention(q, kp, vp, shared, lens, **kw)
+    want = paged_attention(q, *args, table, lens, mask=None, **ex)
+    assert torch.equal(got, want) and torch.isfinite(got).all()
+
+
+def test_chunks_that_do_not_ascend(gpu_lib):
+    """Chunks that overlap, go back or leave the rows: nothing outside the rows is written."""
+    from paper_2502_15572_amd import paged_attention
+    say("attend: odd chunks")
+    c = Case(6, [200] * 5, [7] * 5, 2, 4, 64, 16, "bf16", "bf16", ragged=True)
+    (q, kp, vp, table, lens), kw = c.tensors()
+    for starts in ([0, 35, 0, 35, 0, 35], [35, 20, 10, 5, 2, 0], [-5, 3, 50, 1 << 30, 7, 9],
+                   [0, 0, 0, 0, 0, 1 << 30]):
+        kw["starts"] = torch.tensor(starts, dtype=torch.int32, device=DEV)
+        buf = torch.full((35 + 64, c.H, c.dim), 7.0, dtype=torch.bfloat16, device=DEV)
+        paged_attention(q, kp, vp, table, lens, **kw, out=buf[32:67])
+        torch.cuda.synchronize()
+        assert (buf[:32] == 7).all() and (buf[67:] == 7).all()
+
+
+def test_more_blocks_than_a_launch_takes(gpu_lib):
+    import ctypes
+    from paper_2502_15572_amd import _lib
+    say("attend: too many blocks")
+    need = ctypes.c_int64()
+    c = _lib.KvCache(None, None, None, None, 4, 16, 16, 64, _lib.F16)
+    ask = lambda B: gpu_lib.dresd_paged_attention_workspace(c, 16, 0, 1, B, B, 5,  # noqa: E731
+                                                            ctypes.byref(need))
+    assert ask((1 << 20) - 1) == _lib.OK and need.value == 0
+    assert ask(1 << 20) == _lib.EINVAL
+    assert "blocks" in gpu_lib.dresd_last_error().decode()

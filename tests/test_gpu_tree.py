@@ -119,3 +119,19 @@ def test_accept_unaligned_rows_and_last_token(gpu_lib):
                     assert accept_drafts(x, token, parent, nodes)[2].item() == w, (V, off, w)
                 x.fill_(-float("inf"))
                 assert accept_drafts(x, token, parent, nodes)[2].item() == 0
+
+
+def test_accept_zeros_of_both_signs_and_infinities(gpu_lib):
+    """-0 and +0 tie, +inf is the largest, the first of them wins."""
+    from paper_2502_15572_amd import accept_drafts
+    say("accept: zeros")
+    inf = float("inf")
+    for dtype in (torch.float32, torch.float16, torch.bfloat16):
+        x = torch.full((1, 4, 3000), -1.0, dtype=dtype, device=DEV)
+        x[0, 0, 7], x[0, 0, 2900] = -0.0, 0.0              # -> 7
+        x[0, 1, 1], x[0, 1, 2] = 0.0, -0.0                 # -> 1
+        x[0, 2, 2048], x[0, 2, 2999], x[0, 2, 5] = inf, inf, 60000.0   # -> 2048
+        x[0, 3] = -inf
+        x[0, 3, :9] = float("nan")                         # -> 9
+        path, n, nxt = accept_drafts(x, up([[0, 7, 1, 2048]]), up([[-1, 0, 1, 2]]), up([4]))
+        assert path.tolist() == [[0, 1, 2, 3]] and n.tolist() == [4] and nxt.tolist() == [9]

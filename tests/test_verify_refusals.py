@@ -172,3 +172,18 @@ def test_python_refuses_cpu_tensors_and_wrong_shapes():
                       ((x, tk.long(), tk, n), TypeError), ((x, tk, tk, n[:1]), ValueError)]:
         with pytest.raises(err):
             dresd.accept_drafts(*args)
+
+
+def test_more_than_a_launch_takes():
+    """A launch has fewer than 2^32 threads: 1,024 a query in trees and acceptance, 8, 16 or 32 a
+    row in cache writes and reads."""
+    lib = _lib.load()
+    F = FAKE
+    for B in (1 << 22, (1 << 31) - 1):
+        assert lib.dresd_draft_tree(F, F, F, B, 4, 4, 0, 13, F, F, F, F, F, None) == E
+        assert lib.dresd_accept_drafts(F, 0, 100, 100, F, F, F, B, 4, 4, F, F, F, None) == E
+    for dim, most in ((64, 1 << 29), (72, 1 << 28), (128, 1 << 28), (136, 1 << 27), (256, 1 << 27)):
+        c = cache(dim=dim, heads=2)
+        assert write(lib, c, k_row=2 * dim, k_head=dim, v_row=2 * dim, v_head=dim,
+                     n=most // 2 - 15) == E
+        assert read(lib, c, n=most // 2 - 15) == E
