@@ -182,6 +182,13 @@ __device__ __forceinline__ float value_factor(uint32_t byte, bool masked) {
   return byte != 255u ? __uint_as_float(byte << 23) : masked ? 0.f : __builtin_nanf("");
 }
 
+// What a value row's exponent adds to its score where weights are f16, in powers of two: the
+// largest weight is that of the value as it is stored.
+__device__ __forceinline__ float value_exponent(uint32_t byte) {
+  const int e = (int)byte - 127;
+  return (float)(e < -60 ? -60 : e > 20 ? 20 : e);
+}
+
 // Positions past this are not seen (a tile's stay inside 31 bits).
 constexpr int kPositions = 0x7fffff00;
 

@@ -30,8 +30,9 @@ constexpr int kThreads = 256;
 constexpr int kWaves = 4;
 constexpr int kKeys = 64;
 
-// Of each wave: row offsets [keys] i64, factors of keys and values [keys] f32 each.
-constexpr size_t kWaveBytes = kKeys * 16;
+// Of each wave: row offsets [keys] i64, factors of keys and values, and the values' exponents as
+// a row's maximum takes them, [keys] f32 each.
+constexpr size_t kWaveBytes = kKeys * 20;
 // Whether a key of the tile has a value that is not finite, two tiles.
 constexpr size_t kFlagBytes = 2 * kKeys;
 constexpr size_t tile_bytes(int dp) { return (size_t)kKeys * dp * 2; }
@@ -45,6 +46,10 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) dresd_attend_tile
   constexpr int LR = F8 ? DP / 16 : DP / 8;       // lanes of a row in a load
   constexpr int RP = kThreads / LR;               // rows of a load
   constexpr int NP = kKeys / RP;                  // loads of a tile
+  // Addresses of values in LDS are formed anew for each tile where the compiler, which would
+  // keep them all, runs out of registers (3 sequences of 16,000 tokens and 2,048 new ones, 8 x 4
+  // heads of 256: 8 bits 4.2 ms against 5.7, 16 bits 3.3 against 3.2 to 4.2).
+  constexpr bool kAnew = DP == 256;
   extern __shared__ __align__(16) uint8_t lds[];
   const int tid = threadIdx.x, lane = tid & 63;
   const int wid = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -57,7 +62,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) dresd_attend_tile
   uint8_t *kt = lds, *vt = lds + 2 * tile_bytes(DP);
   uint8_t *mine = lds + 4 * tile_bytes(DP) + (size_t)wid * kWaveBytes;
   int64_t *offs = reinterpret_cast<int64_t *>(mine);
-  float *kf = reinterpret_cast<float *>(offs + kKeys), *vf = kf + kKeys;
+  float *kf = reinterpret_cast<float *>(offs + kKeys), *vf = kf + kKeys, *va = vf + kKeys;
   uint8_t *flags = lds + 4 * tile_bytes(DP) + kWaves * kWaveBytes;
 
   // queries: operand of row 32 wid + col
@@ -199,6 +204,8 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) dresd_attend_tile
       }
     }
     if constexpr (F8) {
+      int sl = tid % LR, sr = tid / LR;
+      if constexpr (kAnew) asm volatile("" : "+v"(sl), "+v"(sr));
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
         const int k = RP * i + sr;
@@ -209,6 +216,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) dresd_attend_tile
       }
       kf[lane] = __uint_as_float(ke << 23);
       vf[lane] = value_factor(ve, masked);
+      if constexpr (QT == kF16) va[lane] = value_exponent(ve);
     }
   };
 
@@ -266,17 +274,13 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) dresd_attend_tile
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        f4 vfac;
+        f4 vexp;
         if constexpr (F8 && QT == kF16)
-          vfac = *reinterpret_cast<const f4 *>(vf + 32 * b + 8 * j + 4 * half);
+          vexp = *reinterpret_cast<const f4 *>(va + 32 * b + 8 * j + 4 * half);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           float x = s[b][4 * j + i];
-          if constexpr (F8 && QT == kF16) {
-            // the largest weight is that of the value as it is stored
-            const int e = (int)((__float_as_uint(vfac[i]) >> 23) & 255u) - 127;
-            x = x * c2 + (float)(e < -60 ? -60 : e > 20 ? 20 : e);
-          }
+          if constexpr (F8 && QT == kF16) x = fmaf(x, c2, vexp[i]);
           top = fmaxf(top, x);
         }
       }
@@ -311,7 +315,9 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) dresd_attend_tile
         }
       }
     l += sum;
-    const int g = (lane >> 4) & 1, i16 = lane & 15, in = (i16 & 1) * 8;
+    int ln = lane;
+    if constexpr (kAnew) asm volatile("" : "+v"(ln));
+    const int g = (ln >> 4) & 1, i16 = ln & 15, in = (i16 & 1) * 8;
     __builtin_amdgcn_s_setprio(1);
     constexpr int kV = 4 * (DP / 32), kVAhead = 4;
     v8 vx[kVAhead + 1];

@@ -322,7 +322,7 @@ __global__ void __launch_bounds__(kThreads, (Ring<F8, DP>::kPair ? 2 : 1)) dresd
     }
 
     // weights
-    f4 vfac[U];
+    f4 vfac[U], vexp[U];
     if constexpr (F8) {
 #pragma unroll
       for (int g = 0; g < U; ++g) {
@@ -331,6 +331,7 @@ __global__ void __launch_bounds__(kThreads, (Ring<F8, DP>::kPair ? 2 : 1)) dresd
 #pragma unroll
           for (int c = 0; c < CT; ++c) s[c][g][e] *= __uint_as_float(kb[g][e] << 23);
           vfac[g][e] = __uint_as_float(vb[g][e] << 23);
+          if constexpr (QT == kF16) vexp[g][e] = value_exponent(vb[g][e]);
         }
       }
     }
@@ -355,11 +356,7 @@ __global__ void __launch_bounds__(kThreads, (Ring<F8, DP>::kPair ? 2 : 1)) dresd
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           float x = s[c][g][e];
-          if constexpr (F8 && QT == kF16) {
-            // the largest weight is that of the value as it is stored
-            const int ex = (int)((__float_as_uint(vfac[g][e]) >> 23) & 255u) - 127;
-            x = x * c2 + (float)(ex < -60 ? -60 : ex > 20 ? 20 : ex);
-          }
+          if constexpr (F8 && QT == kF16) x = fmaf(x, c2, vexp[g][e]);
           top = fmaxf(top, x);
         }
       if constexpr (!(F8 && QT == kF16)) top *= c2;  // (in powers of two)
