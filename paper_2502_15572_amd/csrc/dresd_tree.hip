@@ -16,10 +16,14 @@
 // rows are written whole (a thread per node wrote 8 bytes a row apart).
 //
 // Acceptance.  From node 0, the arg max of the node's logits names the child
-// to go on to.  Only the path's rows are read.  One workgroup per query: what
-// bounds it is one compute unit's reading (about 100 GB/s) and some 2 us of latency
-// a node.  A lane keeps the largest of every 16 bytes and where the first of them
-// began; which of the 16 bytes' elements it was is looked up at the end.
+// to go on to.  Only the path's rows are read, and with each row's last bytes the first of
+// the row of its lowest child (the best draft's): its path needs no wait for them, another one
+// has them read in vain.  One workgroup per query: what bounds it is what one compute unit
+// reads (some 60 GB/s) and 1.8 us a node between rows (8 nodes with rows of 10 KB 15 us, of 250 KB
+// 32, for 64 queries 42; without the rows ahead, with 1,024 threads, which were in each
+// other's way, and fmaxf 28, 48 and 54).  More units a query would have to wait for one another
+// at every node.  A lane keeps the largest of its 16 bytes and which they were; the element
+// among them is looked up at the end.
 #include <algorithm>
 
 #include "dresd_device.h"
@@ -208,145 +212,256 @@ __global__ void __launch_bounds__(kTreeThreads) dresd_tree(TreeParams p) {
   }
 }
 
-constexpr int kAcceptThreads = 1024;
+constexpr int kAcceptThreads = 512;
+constexpr int kAcceptWaves = kAcceptThreads / kWaveSize;
+
+// The largest of three, one instruction.  fmaxf adds one for each operand that may be a signalling
+// NaN, which IEEE mode would let through; without that mode it counts as a quiet one does.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm volatile("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+__device__ __forceinline__ void leave_ieee_mode() {
+  __builtin_amdgcn_s_setreg(1 | 9 << 6, 0);  // register MODE, bit 9, one bit
+}
 
 template <int DT>
 struct Logits;
 template <>
 struct Logits<kF32> {
   static constexpr int kPer = 4;             // elements of 16 bytes
-  static __device__ __forceinline__ float one(const void *x, int64_t at) {
-    return static_cast<const float *>(x)[at];
-  }
-  static __device__ __forceinline__ float largest(u4 x) {
-    return fmaxf(fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])),
-                 fmaxf(__uint_as_float(x[2]), __uint_as_float(x[3])));
-  }
+  typedef float Raw;
+  static __device__ __forceinline__ float value(Raw x) { return x; }
+  static __device__ __forceinline__ float get(u4 x, int e) { return __uint_as_float(x[e]); }
 };
 template <>
 struct Logits<kF16> {
   static constexpr int kPer = 8;
-  static __device__ __forceinline__ float one(const void *x, int64_t at) {
-    return (float)static_cast<const _Float16 *>(x)[at];
-  }
-  static __device__ __forceinline__ float largest(u4 x) {
-    const h8 h = __builtin_bit_cast(h8, x);
-    float m = fmaxf((float)h[0], (float)h[1]);
-#pragma unroll
-    for (int i = 2; i < 8; ++i) m = fmaxf(m, (float)h[i]);
-    return m;
+  typedef _Float16 Raw;
+  static __device__ __forceinline__ float value(Raw x) { return (float)x; }
+  static __device__ __forceinline__ float get(u4 x, int e) {
+    return (float)__builtin_bit_cast(h8, x)[e];
   }
 };
 template <>
 struct Logits<kBF16> {
   static constexpr int kPer = 8;
-  static __device__ __forceinline__ float one(const void *x, int64_t at) {
-    return __uint_as_float((uint32_t)static_cast<const uint16_t *>(x)[at] << 16);
+  typedef uint16_t Raw;
+  static __device__ __forceinline__ float value(Raw x) {
+    return __uint_as_float((uint32_t)x << 16);
   }
-  static __device__ __forceinline__ float largest(u4 x) {
-    float m = -__builtin_huge_valf();
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      m = fmaxf(m, fmaxf(__uint_as_float(x[i] << 16), __uint_as_float(x[i] & 0xffff0000u)));
-    return m;
+  static __device__ __forceinline__ float get(u4 x, int e) {
+    return __uint_as_float(e & 1 ? x[e / 2] & 0xffff0000u : x[e / 2] << 16);
   }
 };
 
-// Ranking key of a place in a row: the larger logit, then the lower place.  Places
-// where no logit was above -inf (NaN among them) rank by the place alone.
-__device__ __forceinline__ uint64_t place_key(float x, int at) {
-  return ((uint64_t)order_bits(x) << 32) | (uint64_t)(~(uint32_t)at);
+// The largest of 16 bytes, NaNs left out (NaN if there is nothing else; outside IEEE mode).
+template <int DT>
+__device__ __forceinline__ float largest(u4 x) {
+  typedef Logits<DT> X;
+  float m;
+  if constexpr (DT == kF32) {
+    m = max3(X::get(x, 0), X::get(x, 1), X::get(x, 2));
+    m = max3(m, X::get(x, 3), m);
+  } else {
+    m = max3(X::get(x, 0), X::get(x, 1), X::get(x, 2));
+    m = max3(m, X::get(x, 3), X::get(x, 4));
+    m = max3(m, X::get(x, 5), X::get(x, 6));
+    m = max3(m, X::get(x, 7), m);
+  }
+  return m;
+}
+
+// The largest of a wave's numbers, for every lane.
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+  auto with = [&](uint32_t y) { x = x > y ? x : y; };
+  with(__builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));  // 1, 2, 4, 8 lanes on in the row
+  with(__builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
+  with(__builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
+  with(__builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
+  with(__builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));  // row 0 to 1, 2 to 3
+  with(__builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));  // rows 0 and 1 to 2 and 3
+  return __builtin_amdgcn_readlane(x, 63);
+}
+
+// The largest of a wave's logits (as order bits) and the lowest place that has it.
+__device__ __forceinline__ void wave_best(uint32_t &x, uint32_t &at) {
+  const uint32_t top = wave_max(x);
+  at = ~wave_max(x == top ? ~at : 0u);
+  x = top;
 }
 
 template <int DT>
 __global__ void __launch_bounds__(kAcceptThreads) dresd_accept(AcceptParams p) {
   typedef Logits<DT> X;
-  constexpr int E = X::kPer, kUnroll = 8;
-  __shared__ uint64_t wbest[kAcceptThreads / kWaveSize];
+  constexpr int E = X::kPer, kElem = 16 / E, kRing = 8;
+  __shared__ uint32_t wtop[kAcceptWaves], wat[kAcceptWaves];
   __shared__ int32_t tok[kNodesMax], par[kNodesMax];
-  __shared__ int32_t child;
+  __shared__ uint32_t heir[kNodesMax];       // lowest child
+  __shared__ uint32_t lowest;
+  __shared__ int32_t now[2];                 // the next node, the present one's token (-1: not known)
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   int nodes = p.nodes[b];
   nodes = nodes < 0 ? 0 : nodes > p.N ? p.N : nodes;
-  if (tid < nodes) {
-    tok[tid] = p.token[(size_t)b * p.N + tid];
-    par[tid] = p.parent[(size_t)b * p.N + tid];
+  leave_ieee_mode();
+
+  // A row: up to the first whole 16 bytes, 16 bytes at a time, the rest.
+  struct Row {
+    const uint8_t *src, *vec;
+    int head, body, tail;
+  };
+  auto row_of = [&](int node) -> Row {
+    Row w;
+    w.src = static_cast<const uint8_t *>(p.logits) + ((int64_t)b * p.N + node) * p.row * kElem;
+    w.head = (int)((16 - ((uintptr_t)w.src & 15)) & 15) / kElem;
+    w.head = w.head < p.V ? w.head : p.V;
+    w.vec = w.src + w.head * kElem;
+    w.body = (p.V - w.head) / E;
+    w.tail = p.V - w.head - w.body * E;
+    return w;
+  };
+  // this thread's element before or past the row's whole 16 bytes (if any, else the first), ...
+  auto edge_at = [&](const Row &w) -> int {
+    return tid < w.head ? tid : tid >= 64 && tid < 64 + w.tail ? p.V - w.tail + tid - 64 : -1;
+  };
+  typename X::Raw edge = 0;
+  auto load_edge = [&](const Row &w) -> typename X::Raw {
+    const int e = edge_at(w);
+    return reinterpret_cast<const typename X::Raw *>(w.src)[e < 0 ? 0 : e];
+  };
+  // ... and its 16 bytes of those from `at` on (past the last those again)
+  u4 v[kRing];
+  auto load = [&](const uint8_t *vec, uint32_t at, uint32_t last) -> u4 {
+    at += (uint32_t)tid * 16;
+    return *reinterpret_cast<const u4 *>(vec + (at < last ? at : last));
+  };
+
+  Row w = row_of(0);
+  bool ready = false;                        // whether the row's first 16 bytes are on their way
+  if (nodes > 0 && w.body > 0) {
+    edge = load_edge(w);
+#pragma unroll
+    for (int k = 0; k < kRing; ++k)
+      v[k] = load(w.vec, k * kAcceptThreads * 16, (uint32_t)(w.body - 1) * 16);
+    ready = true;
   }
+  for (int c = tid; c < nodes; c += kAcceptThreads) {
+    tok[c] = p.token[(size_t)b * p.N + c];
+    par[c] = p.parent[(size_t)b * p.N + c];
+    heir[c] = ~0u;
+  }
+  __syncthreads();
+  for (int c = tid; c < nodes; c += kAcceptThreads)
+    if (par[c] >= 0 && par[c] < c) atomicMin(&heir[par[c]], (uint32_t)c);
+  __syncthreads();
   int u = nodes > 0 ? 0 : -1, done = 0;
   int32_t g = -1;
   while (u >= 0) {
-    if (tid == 0) {
-      p.path[(size_t)b * p.most + done] = u;
-      child = p.N;
+    if (!ready) {
+      edge = load_edge(w);
+      if (w.body > 0)
+#pragma unroll
+        for (int k = 0; k < kRing; ++k)
+          v[k] = load(w.vec, k * kAcceptThreads * 16, (uint32_t)(w.body - 1) * 16);
     }
+    if (tid == 0) p.path[(size_t)b * p.most + done] = u;
     ++done;
-    // the row: up to the first whole 16 bytes, 16 bytes at a time, the rest
-    const int64_t row = ((int64_t)b * p.N + u) * p.row;
-    const uint8_t *at = static_cast<const uint8_t *>(p.logits) + row * (16 / E);
-    int head = (int)((16 - ((uintptr_t)at & 15)) & 15) / (16 / E);
-    head = head < p.V ? head : p.V;
-    const int body = (p.V - head) / E, tail = p.V - head - body * E;
-    const u4 *vec = reinterpret_cast<const u4 *>(at + head * (16 / E));
+    // the row that is read next, if its path is that of the lowest children
+    const int guess = __builtin_amdgcn_readfirstlane(done < p.most ? (int)heir[u] : -1);
+    const Row next = row_of(guess < 0 ? u : guess);
+    const typename X::Raw mine = edge;
     float best = -__builtin_huge_valf();
-    int where = p.V;                         // element at which the best 16 bytes begin
-    for (int c0 = tid; c0 < body; c0 += kUnroll * kAcceptThreads) {
-      u4 v[kUnroll];
+    int which = -1;                          // of this thread's 16 bytes
+    for (int r = 0; r < w.body; r += kRing * kAcceptThreads) {
+      const bool end = r + kRing * kAcceptThreads >= w.body;
+      // (nothing to guess: the row's first bytes again)
+      const uint8_t *from = end ? next.vec : w.vec;
+      const uint32_t at = end ? 0u : (uint32_t)(r + kRing * kAcceptThreads) * 16;
+      const uint32_t last = !end                          ? (uint32_t)(w.body - 1) * 16
+                            : guess < 0 || next.body == 0 ? 0u
+                                                          : (uint32_t)(next.body - 1) * 16;
+      if (end) edge = load_edge(next);
 #pragma unroll
-      for (int k = 0; k < kUnroll; ++k) {    // (past the end the first again, which changes nothing)
-        const int c = c0 + k * kAcceptThreads;
-        v[k] = vec[c < body ? c : c0];
-      }
-#pragma unroll
-      for (int k = 0; k < kUnroll; ++k) {
-        const float m = X::largest(v[k]);
-        if (m > best) {
-          best = m;
-          where = head + (c0 + k * kAcceptThreads) * E;
+      for (int k = 0; k < kRing; ++k) {
+        if (r + k * kAcceptThreads < w.body) {
+          const float m = largest<DT>(v[k]);
+          const bool up = m > best;
+          best = up ? m : best;
+          which = up ? r / kAcceptThreads + k : which;
         }
+        v[k] = load(from, at + k * kAcceptThreads * 16, last);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
-    if (tid < head || (tid >= 64 && tid < 64 + tail)) {
-      const int e = tid < head ? tid : head + body * E + tid - 64;
-      const float m = X::one(at, e);
-      if (m > best || (m == best && e < where && where < p.V)) {
-        best = m;
-        where = e;
+    int where = p.V;                         // element at which the best 16 bytes begin
+    if (which >= 0) {
+      const int c = which * kAcceptThreads + tid;
+      where = w.head + (c < w.body ? c : w.body - 1) * E;
+    }
+    const int e = edge_at(w);
+    const float own = X::value(mine);
+    if (e >= 0 && (own > best || (own == best && e < where && where < p.V))) {
+      best = own;
+      where = e;
+    }
+    uint32_t top = order_bits(best), first = (uint32_t)where;
+    wave_best(top, first);
+    if (lane == 0) {
+      wtop[tid >> 6] = top;
+      wat[tid >> 6] = first;
+    }
+    // the lowest child with a token; children have higher numbers
+    auto child = [&](int32_t token) -> int {
+      if (done < p.most)
+        for (int c0 = u + 1; c0 < nodes; c0 += kWaveSize) {
+          const int c = c0 + lane;
+          const uint64_t hit = __ballot(c < nodes && par[c] == u && tok[c] == token);
+          if (hit) return c0 + __ffsll((long long)hit) - 1;
+        }
+      return -1;
+    };
+    __syncthreads();
+    if (tid < kWaveSize) {                   // (one wave: they would only be in each other's way)
+      top = wtop[lane % kAcceptWaves];
+      first = wat[lane % kAcceptWaves];
+      wave_best(top, first);
+      int32_t is = __builtin_amdgcn_readfirstlane((int)first);
+      if (is >= w.head && is < p.V - w.tail) {
+        // the first of the 16 bytes' elements that has the value (a scalar load, which does not
+        // wait for those under way)
+        typedef const __attribute__((address_space(4))) u4 cu4;
+        const u4 x = *(cu4 *)(uintptr_t)(w.src + (int64_t)is * kElem);
+        const float most = order_value(top);
+        int e0 = 0;
+#pragma unroll
+        for (int e = E - 1; e >= 0; --e) e0 = X::get(x, e) == most ? e : e0;
+        is += __builtin_amdgcn_readfirstlane(e0);
+      }
+      const int to = is < p.V ? child(is) : -1;
+      if (lane == 0) {
+        now[0] = to;
+        now[1] = is < p.V ? is : -1;
+        lowest = p.V;
       }
     }
-    uint64_t key = place_key(best, where);
-#pragma unroll
-    for (int o = 1; o < kWaveSize; o <<= 1) {
-      const uint64_t other = __shfl_xor(key, o, kWaveSize);
-      key = other > key ? other : key;
+    __syncthreads();
+    int to = __builtin_amdgcn_readfirstlane(now[0]);
+    g = __builtin_amdgcn_readfirstlane(now[1]);
+    if (g < 0) {                             // nothing above -inf: the first -inf, else (NaN alone) 0
+      uint32_t low = p.V;
+      for (int e = tid; e < p.V && low == (uint32_t)p.V; e += kAcceptThreads)
+        if (X::value(reinterpret_cast<const typename X::Raw *>(w.src)[e]) == -__builtin_huge_valf())
+          low = e;
+      if (low < (uint32_t)p.V) atomicMin(&lowest, low);
+      __syncthreads();
+      g = lowest < (uint32_t)p.V ? (int)lowest : 0;
+      to = child(g);
+      __syncthreads();
     }
-    if (lane == 0) wbest[tid >> 6] = key;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < kAcceptThreads / kWaveSize; ++w) key = wbest[w] > key ? wbest[w] : key;
-    best = order_value((uint32_t)(key >> 32));
-    where = (int)~(uint32_t)key;
-    if (where < p.V) {
-      // the first of its elements that has the value
-      const bool is = lane < E && where + lane < p.V && X::one(at, where + lane) == best;
-      g = where + __ffsll((long long)__ballot(is)) - 1;
-    } else {
-      // nothing above -inf: the first -inf, else (NaN alone) token 0
-      int low = p.V;
-      for (int e = tid; e < p.V && low == p.V; e += kAcceptThreads)
-        if (X::one(at, e) == -__builtin_huge_valf()) low = e;
-      __syncthreads();
-      if (tid == 0) wbest[0] = (uint64_t)p.V;
-      __syncthreads();
-      if (low < p.V) atomicMin(reinterpret_cast<unsigned long long *>(wbest), (unsigned long long)low);
-      __syncthreads();
-      g = (int)wbest[0] < p.V ? (int)wbest[0] : 0;
-    }
-    // the lowest child with that token; children have higher numbers
-    const int c = u + 1 + tid;               // at most kNodesMax - 1 of them
-    if (done < p.most && c < nodes && par[c] == u && tok[c] == g) atomicMin(&child, c);
-    __syncthreads();
-    u = child < p.N ? child : -1;
-    __syncthreads();
+    u = to;
+    ready = u >= 0 && u == guess && w.body > 0 && next.body > 0;
+    if (u >= 0) w = u == guess ? next : row_of(u);
   }
   for (int e = done + tid; e < p.most; e += kAcceptThreads) p.path[(size_t)b * p.most + e] = -1;
   if (tid == 0) {

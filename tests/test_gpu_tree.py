@@ -135,3 +135,24 @@ def test_accept_zeros_of_both_signs_and_infinities(gpu_lib):
         x[0, 3, :9] = float("nan")                         # -> 9
         path, n, nxt = accept_drafts(x, up([[0, 7, 1, 2048]]), up([[-1, 0, 1, 2]]), up([4]))
         assert path.tolist() == [[0, 1, 2, 3]] and n.tolist() == [4] and nxt.tolist() == [9]
+
+
+@pytest.mark.parametrize("bits,dtype", [(0x7f81, torch.bfloat16), (0xff81, torch.bfloat16),
+                                        (0x7f800001, torch.float32), (0x7d01, torch.float16),
+                                        (0x7fc00000, torch.float32), (0xffff, torch.float16)])
+def test_accept_among_nans(gpu_lib, bits, dtype):
+    """Quiet and signalling NaNs, of either sign, at every place beside the largest logit."""
+    from paper_2502_15572_amd import accept_drafts
+    say("accept: NaN", hex(bits), dtype)
+    V, size = 4099, torch.finfo(dtype).bits // 8
+    raw = {2: torch.int16, 4: torch.int32}[size]
+    nan = torch.tensor([bits], dtype=torch.int64).to(raw).item() if bits < 1 << (8 * size - 1) \
+        else bits - (1 << 8 * size)
+    for hole in range(8):                                  # what is not NaN in every 8 elements
+        for sign in (1.0, -1.0):
+            x = torch.full((1, 2, V), nan, dtype=raw, device=DEV).view(dtype)
+            x[:, :, hole::8] = -2.0
+            x[0, 0, 2048 + hole] = sign
+            x[0, 1, 4088 + hole] = sign * 0.5
+            path, n, nxt = accept_drafts(x, up([[0, 2048 + hole]]), up([[-1, 0]]), up([2]))
+            assert path.tolist() == [[0, 1]] and nxt.tolist() == [4088 + hole]
