@@ -94,6 +94,10 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) dresd_attend_tile
     for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
   float m = -3e38f, l = 0.f;
 
+  // A wave without rows of its own takes part in the copies alone, and leaves the LDS to the others
+  // (trees of 91 nodes, 32 heads: 109 -> 104 us).
+  const bool works = u.row0 + 32 * wid < u.rows;
+
   // this split's tiles
   const int end = reach(pl, u, pl.rows);
   const int tiles = end > 0 ? (end + kKeys - 1) / kKeys : 0;
@@ -363,7 +367,7 @@ __global__ void __launch_bounds__(kThreads, DP <= 128 ? 2 : 1) dresd_attend_tile
         next_masked = (t + 2) * kKeys > plain || next_ok != ~0ull;
       }
       __builtin_amdgcn_sched_barrier(0);
-      compute(buf, t, masked, ok);
+      if (works) compute(buf, t, masked, ok);
       __builtin_amdgcn_sched_barrier(0);
       if (more) store(Other{}, next_masked, next_ok);
       __syncthreads();
