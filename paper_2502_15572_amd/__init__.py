@@ -483,16 +483,25 @@ def _kv_cache(k_pages, v_pages, k_exp, v_exp):
     code = _CACHE_DTYPES.get(k_pages.dtype)
     if code is None:
         raise TypeError("a cache is float16, bfloat16 or float8_e4m3fn, not %s" % k_pages.dtype)
-    P, H, page, D = _expect_dim("k_pages", k_pages, 4)
-    _expect("k_pages", k_pages, k_pages.dtype, P, H, page, D)
-    _expect("v_pages", v_pages, k_pages.dtype, P, H, page, D)
-    if (code == _lib.F8) != (k_exp is not None) or (k_exp is None) != (v_exp is None):
+    P, H, page, D = shape = _expect_dim("k_pages", k_pages, 4)
+    # (one condition where all is well: a call of one token is bound by these checks)
+    if not (v_pages.dtype == k_pages.dtype and v_pages.shape == shape and k_pages.is_contiguous()
+            and v_pages.is_contiguous()):
+        _expect("k_pages", k_pages, k_pages.dtype, P, H, page, D)
+        _expect("v_pages", v_pages, k_pages.dtype, P, H, page, D)
+    if code != _lib.F8:
+        if k_exp is not None or v_exp is not None:
+            raise ValueError("an 8-bit cache has k_exp and v_exp, a 16-bit one neither")
+        return _lib.KvCache(k_pages.data_ptr(), v_pages.data_ptr(), None, None, P, page, H, D, code)
+    if k_exp is None or v_exp is None:
         raise ValueError("an 8-bit cache has k_exp and v_exp, a 16-bit one neither")
-    if k_exp is not None:
-        _expect("k_exp", k_exp, torch.uint8, P, H, page)
-        _expect("v_exp", v_exp, torch.uint8, P, H, page)
-    return _lib.KvCache(k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_exp), _ptr(v_exp), P, page,
-                        H, D, code)
+    u8, exps = torch.uint8, (P, H, page)
+    if not (k_exp.dtype == u8 == v_exp.dtype and k_exp.shape == exps == v_exp.shape
+            and k_exp.is_contiguous() and v_exp.is_contiguous()):
+        _expect("k_exp", k_exp, u8, P, H, page)
+        _expect("v_exp", v_exp, u8, P, H, page)
+    return _lib.KvCache(k_pages.data_ptr(), v_pages.data_ptr(), k_exp.data_ptr(),
+                        v_exp.data_ptr(), P, page, H, D, code)
 
 
 def kv_write(k, v, slots, k_pages, v_pages, k_exp=None, v_exp=None, stream=None) -> None:
