@@ -117,11 +117,11 @@ AttendPlan plan_of(const AttendParams &p, int cus) {
   const int64_t tokens = p.ragged ? (p.T + (p.B > 0 ? p.B : 1) - 1) / (p.B > 0 ? p.B : 1) : p.n;
   const int64_t rows = tokens * pl.group;
   // Up to 32 rows the wave kernel; in 8 bits up to 64, in two blocks, since the tile kernel
-  // converts what it reads before it shares it (64 rows of 8 x 32 heads of 128 over 1,000 to
-  // 4,000 tokens: 8 bits 74 us against 101, 16 bits 107 against 99).  The wave kernel copies 16
-  // bytes at a time.
+  // converts what it reads before it shares it (8 sequences of 1,000 to 4,000 tokens, 32 heads; 64
+  // rows in 8 bits 70 to 75 us against 85 to 90, with heads of 256 167 against 215; 91 rows 106
+  // against 96; 64 rows in 16 bits 104 against 90).  The wave kernel copies 16 bytes at a time.
   const bool f8 = p.c.dtype == kF8;
-  const bool wave = rows <= (f8 && p.c.dim <= 128 ? 64 : 32) && !(f8 && p.c.dim % 16);
+  const bool wave = rows <= (f8 ? 64 : 32) && !(f8 && p.c.dim % 16);
   pl.ct = !wave ? 0 : rows <= 16 ? 1 : 2;
   pl.rows = pl.ct ? 16 * pl.ct : 128;
   pl.blocks = (int)(p.ragged ? p.T * pl.group / pl.rows + p.B

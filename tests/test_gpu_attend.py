@@ -413,3 +413,12 @@ def test_more_blocks_than_a_launch_takes(gpu_lib):
     assert ask((1 << 20) - 1) == _lib.OK and need.value == 0
     assert ask(1 << 20) == _lib.EINVAL
     assert "blocks" in gpu_lib.dresd_last_error().decode()
+
+
+@pytest.mark.parametrize("dtype,cache", [("bf16", "f8"), ("f16", "f8"), ("f16", "f16")])
+@pytest.mark.parametrize("n,dim", [(32, 256), (33, 64), (64, 256), (65, 256), (64, 128), (65, 128),
+                                   (97, 256), (130, 256)])
+def test_where_kernels_meet(gpu_lib, n, dim, dtype, cache):
+    """Numbers of rows on either side of what the launch plan goes by."""
+    say("attend rows", n, dim, dtype, cache)
+    Case(n + dim, [333, 20], [n, n], 2, 1, dim, 16, dtype, cache, "tree").check()
