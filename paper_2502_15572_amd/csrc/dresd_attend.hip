@@ -56,6 +56,7 @@ __global__ void __launch_bounds__(kJoinThreads) dresd_attend_join(AttendPlan pl)
     const int64_t t = r / p.q_heads;
     real = t >= p.starts[0] && t < p.starts[p.B];
   }
+  constexpr int NP = GS == G ? kSplitsMax / G : 1;  // parts of a group
   const float2 *ml = reinterpret_cast<const float2 *>(pl.part_ml);
   float2 own[2];                                 // parts j and j + 32
   float top = -3e38f, l = 0.f;
@@ -65,6 +66,19 @@ __global__ void __launch_bounds__(kJoinThreads) dresd_attend_join(AttendPlan pl)
                                             : float2{-3e38f, 0.f};
     top = fmaxf(top, own[i].x);
   }
+  // the sums are on their way before the weights are known (a part without weight has none: what
+  // is read in their place is not used)
+  f4 y[NP];
+  auto fetch = [&](int d) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int s = GS * i + gs;
+      y[i] = f4{};
+      if (real && s < pl.splits && d < p.c.dim)
+        y[i] = *reinterpret_cast<const f4 *>(pl.part_o + ((int64_t)s * rows + r) * p.c.dim + d);
+    }
+  };
+  fetch(4 * j);
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 32));
   float a[2];
@@ -77,17 +91,15 @@ __global__ void __launch_bounds__(kJoinThreads) dresd_attend_join(AttendPlan pl)
   for (int o = 1; o < 32; o <<= 1) l += __shfl_xor(l, o, 32);
   for (int d0 = 0; d0 < p.c.dim; d0 += 128) {
     const int d = d0 + 4 * j;
+    if (d0 > 0) fetch(d);
     f4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < (GS == G ? kSplitsMax / G : 1); ++i) {
+    for (int i = 0; i < NP; ++i) {
       const int s = GS * i + gs;
       const float w = __shfl(i < 32 / GS ? a[0] : a[1], s & 31, 32);
-      if (s < pl.splits && w != 0.f && d < p.c.dim) {  // (a part without weight has no sums)
-        const f4 y =
-            *reinterpret_cast<const f4 *>(pl.part_o + ((int64_t)s * rows + r) * p.c.dim + d);
+      if (w != 0.f)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] += y[e] * w;
-      }
+        for (int e = 0; e < 4; ++e) x[e] += y[i][e] * w;
     }
     part[g][j] = x;
     __syncthreads();
