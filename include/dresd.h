@@ -493,7 +493,7 @@ dresd_status dresd_paged_attention_workspace(const dresd_kv_cache *cache, int32_
  *             b starts at (b N + u) * row elements, row >= V.
  *   token, parent  device, [B, N] int32, nodes device, [B] int32: the tree
  *             (dresd_draft_tree; nodes outside [0, N] count as the nearer bound).
- *   0 <= B < 2^22 (0 is a no-op); 1 <= N <= DRESD_NODES_MAX; 1 <= V <= 2^30;
+ *   0 <= B < 2^22 (0 is a no-op); 1 <= N <= DRESD_NODES_MAX; 1 <= V <= 2^29;
  *   1 <= most <= DRESD_NODES_MAX.
  *   path      device, [B, most] int32 out: the accepted nodes, -1 past them.
  *   accepted  device, [B] int32 out: their number, >= 1 (0 for an empty tree).

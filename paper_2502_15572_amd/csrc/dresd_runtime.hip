@@ -1477,7 +1477,7 @@ dresd_status dresd_accept_drafts(const void *logits, int32_t dtype, int64_t row,
                                  dresd_stream stream) {
   if (B < 0 || B > kQueriesMax) return fail(DRESD_EINVAL, "B out of range");
   if (dtype < DRESD_F32 || dtype > DRESD_BF16) return fail(DRESD_EINVAL, "unknown dtype");
-  if (V < 1 || V > (1 << 30)) return fail(DRESD_EINVAL, "V out of range");
+  if (V < 1 || V > (1 << 29)) return fail(DRESD_EINVAL, "V out of range");
   if (row < V || row > ((int64_t)1 << 40)) return fail(DRESD_EINVAL, "row out of range");
   if (N < 1 || N > DRESD_NODES_MAX) return fail(DRESD_EINVAL, "N must be in [1, DRESD_NODES_MAX]");
   if (most < 1 || most > DRESD_NODES_MAX)

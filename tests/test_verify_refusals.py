@@ -174,6 +174,13 @@ def test_python_refuses_cpu_tensors_and_wrong_shapes():
             dresd.accept_drafts(*args)
 
 
+def test_rows_of_more_than_31_bits_of_bytes():
+    """Offsets within a row of logits are 32 bits, past its end by what a workgroup reads at once."""
+    lib = _lib.load()
+    F, V = FAKE, (1 << 29) + 1
+    assert lib.dresd_accept_drafts(F, 0, V, V, F, F, F, 1, 4, 4, F, F, F, None) == E
+
+
 def test_more_than_a_launch_takes():
     """A launch has fewer than 2^32 threads: 1,024 a query in trees and acceptance, 8, 16 or 32 a
     row in cache writes and reads."""
