@@ -139,10 +139,16 @@ AttendPlan plan_of(const AttendParams &p, int cus) {
   pl.blocks = (int)(p.ragged ? p.T * pl.group / pl.rows + p.B
                              : (int64_t)p.B * ((rows + pl.rows - 1) / pl.rows));
   const int64_t units = (int64_t)pl.blocks * p.c.heads;
-  // Enough workgroups for every compute unit to hold several, but none without a
-  // round of tiles.
+  // As many workgroups as the compute units hold at once (two each, heads past 128: one), none
+  // without a round of tiles.  Rounded down, since a part of a second round costs what it has fewer
+  // (464 units of up to 282 tokens on 512 places: two splits 20.9 us, one 15.1; drawn shapes 4 to 5%
+  // on average).  Where one split leaves more than a quarter of the places empty, two, if the keys are
+  // many (280 units of up to 12,000 tokens 190 us with one, 154 with two; 264 of 1,900 58
+  // with one, 64 with two).
   const int64_t room = (int64_t)p.width << p.c.page_log;
-  int64_t s = units > 0 ? (2 * (int64_t)cus + units - 1) / units : 1;
+  const int64_t slots = p.c.dim > 128 ? cus : 2 * (int64_t)cus;
+  int64_t s = units > 0 ? slots / units : 1;
+  if (s <= 1 && 4 * units < 3 * slots && room >= 4096) s = 2;
   const int64_t most = (room + 127) / 128;
   s = s < most ? s : most;
   pl.splits = (int)(s < 1 ? 1 : s < kSplitsMax ? s : kSplitsMax);
