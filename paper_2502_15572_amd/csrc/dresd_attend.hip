@@ -149,6 +149,10 @@ AttendPlan plan_of(const AttendParams &p, int cus) {
   const int64_t slots = p.c.dim > 128 ? cus : 2 * (int64_t)cus;
   int64_t s = units > 0 ? slots / units : 1;
   if (s <= 1 && 4 * units < 3 * slots && room >= 4096) s = 2;
+  // Few rows over few keys: reading them alone takes what a second launch takes (8 x 4 heads of 128:
+  // 300 tokens 10.8 us with one split, 10.6 with three; 200 10.2 against 10.9, 450 12.4 against
+  // 11.1), and the caller's thread is done after one.
+  if (pl.ct == 1 && room <= 320) s = 1;
   const int64_t most = (room + 127) / 128;
   s = s < most ? s : most;
   pl.splits = (int)(s < 1 ? 1 : s < kSplitsMax ? s : kSplitsMax);
