@@ -42,9 +42,9 @@ constexpr int kJoinThreads = 256;
 constexpr int64_t kGroupsMax = (1 << 24) - 8;  // workgroups of 256 threads: a launch has fewer than 2^32
 
 // Joins the parts of every row and head: `GS` 32-lane groups of a workgroup a row, of
-// which each takes every GS-th part, four dims a lane (the dims past 128 in a second
-// turn), and whose sums meet in LDS.
-template <int QT, int GS>
+// which each takes every GS-th part, `NP` of them at most and all on their way at once, four dims
+// a lane (the dims past 128 in a second turn), and whose sums meet in LDS.
+template <int QT, int GS, int NP>
 __global__ void __launch_bounds__(kJoinThreads) dresd_attend_join(AttendPlan pl) {
   constexpr int G = kJoinThreads / 32;
   __shared__ f4 part[G][32];
@@ -56,7 +56,6 @@ __global__ void __launch_bounds__(kJoinThreads) dresd_attend_join(AttendPlan pl)
     const int64_t t = r / p.q_heads;
     real = t >= p.starts[0] && t < p.starts[p.B];
   }
-  constexpr int NP = GS == G ? kSplitsMax / G : 1;  // parts of a group
   const float2 *ml = reinterpret_cast<const float2 *>(pl.part_ml);
   float2 own[2];                                 // parts j and j + 32
   float top = -3e38f, l = 0.f;
@@ -96,13 +95,15 @@ __global__ void __launch_bounds__(kJoinThreads) dresd_attend_join(AttendPlan pl)
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int s = GS * i + gs;
-      const float w = __shfl(i < 32 / GS ? a[0] : a[1], s & 31, 32);
+      const float w = __shfl(GS * NP <= 32 || i < 32 / GS ? a[0] : a[1], s & 31, 32);
       if (w != 0.f)
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] += y[i][e] * w;
     }
-    part[g][j] = x;
-    __syncthreads();
+    if constexpr (GS > 1) {
+      part[g][j] = x;
+      __syncthreads();
+    }
     if (real && gs == 0 && d < p.c.dim) {
 #pragma unroll
       for (int i = 1; i < GS; ++i)
@@ -110,15 +111,16 @@ __global__ void __launch_bounds__(kJoinThreads) dresd_attend_join(AttendPlan pl)
         for (int e = 0; e < 4; ++e) x[e] += part[g + i][j][e];
       finish_row<QT>(p, r, d, x, top, l);
     }
-    __syncthreads();
+    if constexpr (GS > 1) __syncthreads();
   }
 }
 
 template <int QT>
 const void *join_kernel(int groups) {
-  return groups == 2   ? (const void *)dresd_attend_join<QT, 2>
-         : groups == 4 ? (const void *)dresd_attend_join<QT, 4>
-                       : (const void *)dresd_attend_join<QT, 8>;
+  return groups == 1   ? (const void *)dresd_attend_join<QT, 1, 2>
+         : groups == 2 ? (const void *)dresd_attend_join<QT, 2, 2>
+         : groups == 4 ? (const void *)dresd_attend_join<QT, 4, 4>
+                       : (const void *)dresd_attend_join<QT, 8, 8>;
 }
 
 AttendPlan plan_of(const AttendParams &p, int cus) {
@@ -186,8 +188,9 @@ hipError_t launch_attend(const AttendParams &p, int cus, hipStream_t st) {
   hipError_t e = hipLaunchKernel((const void *)k, dim3((unsigned)((pl.total + 7) / 8 * 8)),
                                  dim3(256), args, lds, st);
   if (e != hipSuccess || pl.splits == 1) return e;
-  // up to 8 parts are read at once
-  const int groups = pl.splits <= 2 ? 2 : pl.splits <= 4 ? 4 : 8;
+  // few parts: more rows a workgroup (10 parts by four groups 39.4 us of a call, by eight 42.7; two by
+  // one group 102.5, by two 105.5)
+  const int groups = pl.splits <= 2 ? 1 : pl.splits <= 4 ? 2 : pl.splits <= 16 ? 4 : 8;
   const void *j = p.dtype == kF16 ? join_kernel<kF16>(groups) : join_kernel<kBF16>(groups);
   const int64_t rows = p.T * p.q_heads, per = kJoinThreads / 32 / groups;
   return hipLaunchKernel(j, dim3((unsigned)((rows + per - 1) / per)), dim3(kJoinThreads), args, 0,
