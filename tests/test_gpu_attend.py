@@ -422,3 +422,26 @@ def test_where_kernels_meet(gpu_lib, n, dim, dtype, cache):
     """Numbers of rows on either side of what the launch plan goes by."""
     say("attend rows", n, dim, dtype, cache)
     Case(n + dim, [333, 20], [n, n], 2, 1, dim, 16, dtype, cache, "tree").check()
+
+
+@pytest.mark.parametrize("n,words", [(70, 1), (5, 3), (1, 1), (130, 2), (64, 2)])
+@pytest.mark.parametrize("dtype,cache", [("f16", "f16"), ("bf16", "f8")])
+def test_mask_words(gpu_lib, n, words, dtype, cache):
+    """More words than the chunk has bits (whose further ones are set), and fewer."""
+    say("attend: mask words", n, words, dtype, cache)
+    c = Case(n + words, [90, 0], [n, n], 2, 2, 64, 16, dtype, cache, "any")
+    full = np.full((c.T, max(words, c.mask.shape[1])), ~np.uint64(0))
+    full[:, :c.mask.shape[1]] = c.mask
+    if words < c.mask.shape[1]:
+        full[:, words:] = 0
+    c.mask = full                                          # what the oracle looks at
+    (q, kp, vp, table, lens), kw = c.tensors()
+    kw["mask"] = kw["mask"][..., :words].contiguous()
+    from paper_2502_15572_amd import paged_attention
+    out, lse = paged_attention(q, kp, vp, table, lens, **kw, with_lse=True)
+    c.compare(out, lse)
+
+
+def test_a_page_of_65536_tokens(gpu_lib):
+    say("attend: one large page")
+    Case(3, [5000, 64], [3, 3], 1, 2, 64, 65536, "bf16", "bf16").check()
