@@ -397,7 +397,7 @@ def _on(stream, *tensors):
         if stream.device.index != index:
             raise ValueError("the stream must be on the tensors' device")
         return torch.cuda.stream(stream)
-    if index != torch.cuda.current_device():
+    if index != torch._C._cuda_getDevice():
         return torch.cuda.device(index)
     return _HERE
 
@@ -428,11 +428,6 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _stride(t, d):
-    """Stride of a dimension (0 where it is never taken)."""
-    return t.stride(d) if t.shape[d] > 1 else 0
-
-
 def draft_tree(drafts, count, next_tok, nodes: int | None = None, eos: int = 0, out=None,
                stream=None):
     """Prefix tree of each query's drafts (Section 3.6), the tokens that one
@@ -458,7 +453,7 @@ def draft_tree(drafts, count, next_tok, nodes: int | None = None, eos: int = 0, 
     with _on(stream, drafts, count, next_tok, *(out or ())):
         if out is None:
             out = (*drafts.new_empty((3, B, N)).unbind(),
-                   drafts.new_empty((B, N, W), dtype=torch.int64), drafts.new_empty((B,)))
+                   drafts.new_empty((B, N, W), dtype=torch.int64), torch.empty_like(count))
         else:
             for name, t in zip(("token", "parent", "depth"), out):
                 _expect(name, t, i32, B, N)
@@ -514,19 +509,26 @@ def kv_write(k, v, slots, k_pages, v_pages, k_exp=None, v_exp=None, stream=None)
     row's values are the stored ones times 2 ** (exp - 127).  Tokens whose slot
     is outside the cache (-1, say) are skipped; two tokens must not share a slot."""
     import torch
-    if k.dim() != 3 or k.shape != v.shape or k.dtype != v.dtype:
+    shape = k.shape
+    if len(shape) != 3 or shape != v.shape or k.dtype != v.dtype:
         raise ValueError("k and v must be [n, heads, dim] of one type")
-    n = int(k.shape[0])
+    n, heads, dim = shape
     cache = _kv_cache(k_pages, v_pages, k_exp, v_exp)
-    if k.shape[1] != cache.heads or k.shape[2] != cache.dim:
+    if heads != cache.heads or dim != cache.dim:
         raise ValueError("k and v must be [n, %d, %d]" % (cache.heads, cache.dim))
-    if k.stride(2) != 1 or v.stride(2) != 1:
+    kr, kh, kd = k.stride()
+    vr, vh, vd = v.stride()
+    if kd != 1 or vd != 1:
         raise ValueError("the last dimension of k and v must be contiguous")
+    if n < 2:                  # (strides that are never taken)
+        kr = vr = 0
+    if heads < 2:
+        kh = vh = 0
     _expect("slots", slots, torch.int64, n)
     with _on(stream, k, v, slots, k_pages, v_pages, k_exp, v_exp):
         _lib.check(_lib.load().dresd_kv_write(
-            cache, k.data_ptr(), _stride(k, 0), _stride(k, 1), v.data_ptr(), _stride(v, 0),
-            _stride(v, 1), _dtype_code(k), slots.data_ptr(), n, _current(k)))
+            cache, k.data_ptr(), kr, kh, v.data_ptr(), vr, vh, _dtype_code(k), slots.data_ptr(), n,
+            _current(k)))
 
 
 def kv_read(slots, k_pages, v_pages, k_exp=None, v_exp=None, dtype=None, out=None, stream=None):
@@ -542,8 +544,8 @@ def kv_read(slots, k_pages, v_pages, k_exp=None, v_exp=None, dtype=None, out=Non
         dtype = torch.bfloat16 if cache.dtype == _lib.F8 else k_pages.dtype
     with _on(stream, slots, k_pages, v_pages, k_exp, v_exp, *(out or ())):
         if out is None:
-            shape = (n, cache.heads, cache.dim)
-            out = (slots.new_empty(shape, dtype=dtype), slots.new_empty(shape, dtype=dtype))
+            k = slots.new_empty((n, cache.heads, cache.dim), dtype=dtype)
+            out = (k, torch.empty_like(k))
         else:
             _expect("k", out[0], dtype, n, cache.heads, cache.dim)
             _expect("v", out[1], dtype, n, cache.heads, cache.dim)
@@ -588,21 +590,25 @@ def paged_attention(q, k_pages, v_pages, table, lengths, starts=None, mask=None,
     _expect("table", table, torch.int32, B, width)
     if q.dtype not in (torch.float16, torch.bfloat16):
         raise TypeError("q must be float16 or bfloat16, not %s" % q.dtype)
+    shape, strides = q.shape, q.stride()
     if starts is None:
-        if q.dim() != 4 or q.shape[0] != B:
+        if len(shape) != 4 or shape[0] != B:
             raise ValueError("without starts q must be [%d, n, q_heads, dim]" % B)
-        n = int(q.shape[1])
-        T, row = B * n, _stride(q, 1 if n > 1 else 0)
-        if n > 1 and B > 1 and q.stride(0) != n * q.stride(1):
+        n = shape[1]
+        T, row = B * n, strides[1 if n > 1 else 0]
+        if n > 1 and B > 1 and strides[0] != n * strides[1]:
             raise ValueError("q's tokens must be evenly spaced")
     else:
         _expect("starts", starts, torch.int32, B + 1)
-        if q.dim() != 3:
+        if len(shape) != 3:
             raise ValueError("with starts q must be [T, q_heads, dim]")
-        n, T, row = 0, int(q.shape[0]), _stride(q, 0)
-    H = int(q.shape[-2])
-    if q.shape[-1] != cache.dim or q.stride(-1) != 1:
+        n, T, row = 0, shape[0], strides[0]
+    H = shape[-2]
+    if shape[-1] != cache.dim or strides[-1] != 1:
         raise ValueError("q's last dimension must be %d contiguous elements" % cache.dim)
+    head = strides[-2] if H > 1 else 0           # (0: a stride that is never taken)
+    if T < 2:
+        row = 0
     words = 0
     if mask is not None:
         words = _expect_dim("mask", mask, q.dim() - 1)[-1]
@@ -626,7 +632,7 @@ def paged_attention(q, k_pages, v_pages, table, lengths, starts=None, mask=None,
                                     cache.dim, cache.dtype, H, starts is not None, n, B, T, width)
         work = q.new_empty((need,), dtype=torch.uint8) if need else None
         _lib.check(lib.dresd_paged_attention(
-            cache, q.data_ptr(), row, _stride(q, -2), _dtype_code(q), H, _ptr(starts), n, B, T,
+            cache, q.data_ptr(), row, head, _dtype_code(q), H, _ptr(starts), n, B, T,
             table.data_ptr(), width, lengths.data_ptr(), _ptr(mask), words, float(scale),
             o.data_ptr(), _ptr(lse), _ptr(work), need, _current(q)))
     return (o, lse) if with_lse else o
@@ -645,8 +651,9 @@ def accept_drafts(logits, token, parent, nodes, most: int | None = None, out=Non
     if logits.dim() != 3:
         raise ValueError("logits must be [B, N, V]")
     B, N, V = logits.shape
-    row = _stride(logits, 1 if N > 1 else 0)
-    if logits.stride(2) != 1 and V > 1 or (N > 1 and B > 1 and logits.stride(0) != N * row):
+    sb, sn, sv = logits.stride()
+    row = sn if N > 1 else sb if B > 1 else 0    # (0: a stride that is never taken)
+    if sv != 1 and V > 1 or (N > 1 and B > 1 and sb != N * row):
         raise ValueError("the rows of logits must be contiguous and evenly spaced")
     _expect("token", token, i32, B, N)
     _expect("parent", parent, i32, B, N)
