@@ -124,7 +124,7 @@ __device__ __forceinline__ uint32_t lds_address(const uint8_t *p) {
 // Callers wait with wait_vmcnt.
 __device__ __forceinline__ void copy16_from(const uint8_t *src, uint32_t lds) {
   asm volatile(
-      "s_mov_b32 m0, %1\n\t"
+      "s_mov_b32 m0, %1\n\ts_nop 0\n\t"
       "global_load_lds_dwordx4 %0, off"
       :
       : "v"(src), "s"(lds)
@@ -132,7 +132,7 @@ __device__ __forceinline__ void copy16_from(const uint8_t *src, uint32_t lds) {
 }
 __device__ __forceinline__ void copy16_past(const uint8_t *src, uint32_t lds) {
   asm volatile(
-      "s_mov_b32 m0, %1\n\t"
+      "s_mov_b32 m0, %1\n\ts_nop 0\n\t"
       "global_load_lds_dwordx4 %0, off nt"
       :
       : "v"(src), "s"(lds)
@@ -140,7 +140,7 @@ __device__ __forceinline__ void copy16_past(const uint8_t *src, uint32_t lds) {
 }
 __device__ __forceinline__ void copy_byte_from(const uint8_t *src, uint32_t lds) {
   asm volatile(
-      "s_mov_b32 m0, %1\n\t"
+      "s_mov_b32 m0, %1\n\ts_nop 0\n\t"
       "global_load_lds_ubyte %0, off"
       :
       : "v"(src), "s"(lds)

@@ -45,10 +45,12 @@ __device__ __forceinline__ void wave_sync_lds() {
 // assembly so that the compiler's wait-count model, which cannot tell which
 // LDS bytes such a copy writes, adds no waits for them before unrelated LDS
 // reads.  Callers wait with wait_vmcnt before reading the destination.
+// A copy may read M0 one wait state after a scalar write of it, no sooner (it would land at the
+// place of the copy before); the compiler sees to that in its own code, not in such a block.
 __device__ __forceinline__ void copy1_to_lds(const void *src, uint32_t lds) {
   // one dword per lane from its own address; lane l lands at lds + 4 l
   asm volatile(
-      "s_mov_b32 m0, %1\n\t"
+      "s_mov_b32 m0, %1\n\ts_nop 0\n\t"
       "global_load_lds_dword %0, off"
       :
       : "v"(src), "s"(lds)

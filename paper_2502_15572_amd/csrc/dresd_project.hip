@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(256) dresd_project_operand(ProjectParams p) {
 // As copy16_to_lds, 16 or 4 bytes per lane, streamed past the cache.
 __device__ __forceinline__ void copy16_nt_to_lds(const void *base, uint32_t off, uint32_t lds) {
   asm volatile(
-      "s_mov_b32 m0, %2\n\t"
+      "s_mov_b32 m0, %2\n\ts_nop 0\n\t"
       "global_load_lds_dwordx4 %0, %1 nt"
       :
       : "v"(off), "s"(base), "s"(lds)
@@ -97,7 +97,7 @@ __device__ __forceinline__ void copy16_nt_to_lds(const void *base, uint32_t off,
 }
 __device__ __forceinline__ void copy4_nt_to_lds(const void *base, uint32_t off, uint32_t lds) {
   asm volatile(
-      "s_mov_b32 m0, %2\n\t"
+      "s_mov_b32 m0, %2\n\ts_nop 0\n\t"
       "global_load_lds_dword %0, %1 nt"
       :
       : "v"(off), "s"(base), "s"(lds)

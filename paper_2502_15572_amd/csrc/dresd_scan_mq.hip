@@ -104,9 +104,9 @@ __device__ __forceinline__ u4 query_chunk_mq(const float *q, int d, int B, int c
 __device__ __forceinline__ void copy2_to_lds(const void *src, uint32_t voff0, uint32_t voff1,
                                              uint32_t lds) {
   asm volatile(
-      "s_mov_b32 m0, %3\n\t"
+      "s_mov_b32 m0, %3\n\ts_nop 0\n\t"
       "global_load_lds_dwordx4 %0, %2 nt\n\t"
-      "s_add_u32 m0, m0, 0x400\n\t"
+      "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
       "global_load_lds_dwordx4 %1, %2 nt"
       :
       : "v"(voff0), "v"(voff1), "s"(src), "s"(lds)
@@ -805,14 +805,14 @@ template <bool NT>
 __device__ __forceinline__ void copy_block_to_lds(const void *src, uint32_t voff, uint32_t lds) {
   if constexpr (NT) {
     asm volatile(
-        "s_mov_b32 m0, %2\n\t"
+        "s_mov_b32 m0, %2\n\ts_nop 0\n\t"
         "global_load_lds_dwordx4 %0, %1 nt"
         :
         : "v"(voff), "s"(src), "s"(lds)
         : "memory");
   } else {
     asm volatile(
-        "s_mov_b32 m0, %2\n\t"
+        "s_mov_b32 m0, %2\n\ts_nop 0\n\t"
         "global_load_lds_dwordx4 %0, %1"
         :
         : "v"(voff), "s"(src), "s"(lds)

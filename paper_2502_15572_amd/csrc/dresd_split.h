@@ -35,7 +35,7 @@ __device__ __forceinline__ void split3(float x, uint16_t &a, uint16_t &b, uint16
 // times the lane; see copy1_to_lds.
 __device__ __forceinline__ void copy16_to_lds(const void *base, uint32_t off, uint32_t lds) {
   asm volatile(
-      "s_mov_b32 m0, %2\n\t"
+      "s_mov_b32 m0, %2\n\ts_nop 0\n\t"
       "global_load_lds_dwordx4 %0, %1"
       :
       : "v"(off), "s"(base), "s"(lds)
