@@ -101,6 +101,7 @@ __device__ __forceinline__ u4 query_chunk_mq(const float *q, int d, int B, int c
 // that the compiler's wait-count model, which does not know which LDS bytes
 // an LDS-DMA copy writes, adds no waits for these copies before unrelated LDS
 // reads; the caller waits with wait_vmcnt and a barrier before reading them.
+// The sum sets the carry bit, which the compiler may hold half of an address sum in.
 __device__ __forceinline__ void copy2_to_lds(const void *src, uint32_t voff0, uint32_t voff1,
                                              uint32_t lds) {
   asm volatile(
@@ -110,7 +111,7 @@ __device__ __forceinline__ void copy2_to_lds(const void *src, uint32_t voff0, ui
       "global_load_lds_dwordx4 %1, %2 nt"
       :
       : "v"(voff0), "v"(voff1), "s"(src), "s"(lds)
-      : "memory");
+      : "memory", "scc");
 }
 
 }  // namespace
