@@ -643,18 +643,19 @@ def accept_drafts(logits, token, parent, nodes, most: int | None = None, out=Non
     [B]) by the model's own greedy tokens: from node 0, on to the child that holds
     the token of the node's largest logit (ties to the lower token), while there
     is one and fewer than ``most`` (default N) nodes are accepted.  ``logits``
-    [B, N, V] float32, float16 or bfloat16, rows evenly spaced.  Returns (path [B,
-    most] int32: the accepted nodes, then -1; accepted [B] int32: their number;
-    next_tok [B] int32: the model's token after the last of them)."""
+    [B, N, V] float32, float16 or bfloat16, rows evenly spaced and apart (slices of
+    padded rows need no copy, expanded ones do).  Returns (path [B, most] int32:
+    the accepted nodes, then -1; accepted [B] int32: their number; next_tok [B]
+    int32: the model's token after the last of them)."""
     import torch
     i32 = torch.int32
     if logits.dim() != 3:
         raise ValueError("logits must be [B, N, V]")
     B, N, V = logits.shape
     sb, sn, sv = logits.stride()
-    row = sn if N > 1 else sb if B > 1 else 0    # (0: a stride that is never taken)
-    if sv != 1 and V > 1 or (N > 1 and B > 1 and sb != N * row):
-        raise ValueError("the rows of logits must be contiguous and evenly spaced")
+    row = V if B * N < 2 else sn if N > 1 else sb    # (one row: its stride is never taken)
+    if sv != 1 and V > 1 or row < V or (N > 1 and B > 1 and sb != N * row):
+        raise ValueError("the rows of logits must be contiguous, evenly spaced and apart")
     _expect("token", token, i32, B, N)
     _expect("parent", parent, i32, B, N)
     _expect("nodes", nodes, i32, B)
@@ -667,7 +668,7 @@ def accept_drafts(logits, token, parent, nodes, most: int | None = None, out=Non
             _expect("accepted", out[1], i32, B)
             _expect("next_tok", out[2], i32, B)
         _lib.check(_lib.load().dresd_accept_drafts(
-            logits.data_ptr(), _dtype_code(logits), max(row, V), V, token.data_ptr(),
+            logits.data_ptr(), _dtype_code(logits), row, V, token.data_ptr(),
             parent.data_ptr(), nodes.data_ptr(), B, N, most, *(t.data_ptr() for t in out),
             _current(logits)))
     return tuple(out)

@@ -1,0 +1,38 @@
+"""Batch verification's arguments as the binding hands them on: strides and shapes that the kernels
+would read otherwise are refused before any device work (CPU only)."""
+import pytest
+import torch
+
+import paper_2502_15572_amd as dresd
+
+
+def tree(B, N):
+    t = torch.zeros(B, N, dtype=torch.int32)
+    return t, t, torch.ones(B, dtype=torch.int32)
+
+
+@pytest.mark.parametrize("make", [
+    lambda: torch.zeros(100).expand(2, 3, 100),                        # strides (0, 0, 1)
+    lambda: torch.zeros(1, 1, 100).expand(1, 3, 100),
+    lambda: torch.zeros(2, 1, 100).expand(2, 3, 100),                  # of the nodes alone
+    lambda: torch.zeros(1, 1, 100).expand(4, 1, 100),                  # of the batch, one node
+    lambda: torch.zeros(1, 3, 100).expand(2, 3, 100),
+    lambda: torch.zeros(200).unfold(0, 100, 50).unsqueeze(0),          # rows that overlap
+    lambda: torch.zeros(600).as_strided((2, 3, 100), (297, 99, 1)),
+], ids=range(7))
+def test_rows_of_logits_closer_than_their_length(make):
+    x = make()
+    with pytest.raises(ValueError, match="rows of logits"):
+        dresd.accept_drafts(x, *tree(*x.shape[:2]))
+
+
+@pytest.mark.parametrize("make", [
+    lambda: torch.zeros(2, 3, 100), lambda: torch.zeros(2, 3, 128)[:, :, :100],
+    lambda: torch.zeros(1, 1, 100).as_strided((1, 1, 100), (0, 0, 1)),  # strides never taken
+    lambda: torch.zeros(4, 5, 100)[:, 2:3], lambda: torch.zeros(3, 5, 100)[1:2, :2],
+    lambda: torch.zeros(2, 3, 1).expand(2, 3, 1),
+], ids=range(6))
+def test_rows_of_logits_apart(make):
+    x = make()
+    with pytest.raises(TypeError, match="GPU"):                        # (all that is wrong here)
+        dresd.accept_drafts(x, *tree(*x.shape[:2]))
