@@ -612,6 +612,8 @@ def paged_attention(q, k_pages, v_pages, table, lengths, starts=None, mask=None,
     words = 0
     if mask is not None:
         words = _expect_dim("mask", mask, q.dim() - 1)[-1]
+        if words < 1:          # (an empty tensor has no address, which is no mask)
+            raise ValueError("mask must have a word a row at least")
         _expect("mask", mask, torch.int64, *q.shape[:-2], words)
     if scale is None:
         scale = cache.dim ** -0.5

@@ -36,3 +36,17 @@ def test_rows_of_logits_apart(make):
     x = make()
     with pytest.raises(TypeError, match="GPU"):                        # (all that is wrong here)
         dresd.accept_drafts(x, *tree(*x.shape[:2]))
+
+
+def test_a_mask_without_words():
+    """Its pointer is null, which the C entry takes as no mask."""
+    q = torch.zeros(2, 3, 4, 64, dtype=torch.float16)
+    kp = torch.zeros(3, 2, 16, 64, dtype=torch.float16)
+    table, lengths = torch.zeros(2, 1, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    mask = torch.zeros(2, 3, 0, dtype=torch.int64)
+    with pytest.raises(ValueError, match="word"):
+        dresd.paged_attention(q, kp, kp, table, lengths, mask=mask)
+    starts = torch.tensor([0, 3, 6], dtype=torch.int32)
+    with pytest.raises(ValueError, match="word"):
+        dresd.paged_attention(q.flatten(0, 1), kp, kp, table, lengths, starts=starts,
+                              mask=mask.flatten(0, 1))
