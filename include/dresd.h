@@ -464,9 +464,12 @@ dresd_status dresd_kv_read(const dresd_kv_cache *cache, const int64_t *slots, in
  *             reads no device memory).  Used by this call alone until `stream`
  *             has completed it; its contents do not matter.
  * What masked positions hold does not matter, infinities and NaN included; a row that
- * sees a key or a value that is not finite may become NaN throughout.
+ * sees a key that is not finite, a value past 2^88 or a score outside fp32's range
+ * may become NaN throughout.
  * Scores, softmax statistics and sums are fp32; keys and queries enter the
- * matrix cores unrounded, a row's weights rounded to dtype.  Deterministic.
+ * matrix cores unrounded, a row's weights rounded to dtype (f16 over 8 bits: times
+ * the power of two of their value; less than 2^-35 of the row's largest is lost).
+ * Deterministic.
  * Errors: EINVAL (null pointer with T > 0, ranges, alignment, dtypes that do not
  * fit, too little workspace, more than some 2^24 blocks of the 16 to 128 rows of a
  * cache head that are computed together), EDEVICE.

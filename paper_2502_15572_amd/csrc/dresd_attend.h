@@ -183,10 +183,13 @@ __device__ __forceinline__ float value_factor(uint32_t byte, bool masked) {
 }
 
 // What a value row's exponent adds to its score where weights are f16, in powers of two: the
-// largest weight is that of the value as it is stored.
+// reference goes by the weight of the value as it is stored, which then stays below 2^15.  Between
+// -60 (values that small are zero in f16) and 80 (values of 2^88): there the row's own weight in
+// the sum is 2^-70 at least, and 2^31 weights that exponentials flush, each below 2^-126,
+// are still 2^-25 of it.
 __device__ __forceinline__ float value_exponent(uint32_t byte) {
   const int e = (int)byte - 127;
-  return (float)(e < -60 ? -60 : e > 20 ? 20 : e);
+  return (float)(e < -60 ? -60 : e > 80 ? 80 : e);
 }
 
 // Positions past this are not seen (a tile's stay inside 31 bits).
