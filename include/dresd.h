@@ -407,8 +407,9 @@ typedef struct {
  * elements rounded to nearest even (but down where 2^128 would result);
  * infinite elements are stored as NaN, as NaNs are, and do not take part in
  * the largest magnitude.  A power of two scales without rounding, so rows read
- * back in bf16 or fp32 are exactly the stored ones, and writing them again
- * stores the same values.
+ * back in fp32 are exactly the stored ones, and those with exponents of -124 and up
+ * (magnitudes past 2^-116) in bf16 too, whose smallest number is 2^-133; writing
+ * such rows again stores the same values.
  * Errors: EINVAL (null pointer with n > 0, ranges, alignment, a dtype that does
  * not fit), EDEVICE.
  */

@@ -535,7 +535,7 @@ def kv_read(slots, k_pages, v_pages, k_exp=None, v_exp=None, dtype=None, out=Non
     """Keys and values of cache slots (int64 [n], any order, repeats allowed;
     zeros for a slot outside the cache) as (k, v) [n, heads, dim] in ``dtype``
     (float32, float16 or bfloat16; default: the cache's, bfloat16 for 8-bit caches,
-    which holds their values exactly)."""
+    which holds the values of their rows past 2 ** -116 exactly)."""
     import torch
     cache = _kv_cache(k_pages, v_pages, k_exp, v_exp)
     n, = _expect_dim("slots", slots, 1)

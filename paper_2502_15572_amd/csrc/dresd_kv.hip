@@ -8,7 +8,8 @@
 // and stores e4m3(x 2^-e), rounded to nearest even, and e + 127.  e4m3 is a
 // floating type: its relative step is the same at every power of two, so a power
 // of two costs no precision against amax / 448 and scales without rounding.
-// A row read back is exact in bf16 and fp32, and writing it again stores the same values.
+// A row read back is exact in fp32, and from e = -124 on in bf16 (its smallest code times 2^e is
+// 2^(e - 9), bf16's smallest number 2^-133); writing it again stores the same values.
 //
 // What bounds both is memory: every element is read once and written once.  A
 // lane carries 8 elements (16 bytes of a 16-bit row); the 8, 16 or 32 lanes of a row
