@@ -375,12 +375,13 @@ __global__ void __launch_bounds__(kAcceptThreads) dresd_accept(AcceptParams p) {
     int which = -1;                          // of this thread's 16 bytes
     for (int r = 0; r < w.body; r += kRing * kAcceptThreads) {
       const bool end = r + kRing * kAcceptThreads >= w.body;
-      // (nothing to guess: the row's first bytes again)
-      const uint8_t *from = end ? next.vec : w.vec;
+      // (nothing to guess, or a row without whole 16 bytes: this row's first bytes again)
+      const bool ahead = end && guess >= 0 && next.body > 0;
+      const uint8_t *from = ahead ? next.vec : w.vec;
       const uint32_t at = end ? 0u : (uint32_t)(r + kRing * kAcceptThreads) * 16;
-      const uint32_t last = !end                          ? (uint32_t)(w.body - 1) * 16
-                            : guess < 0 || next.body == 0 ? 0u
-                                                          : (uint32_t)(next.body - 1) * 16;
+      const uint32_t last = ahead  ? (uint32_t)(next.body - 1) * 16
+                            : !end ? (uint32_t)(w.body - 1) * 16
+                                   : 0u;
       if (end) edge = load_edge(next);
 #pragma unroll
       for (int k = 0; k < kRing; ++k) {
