@@ -428,6 +428,12 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _too_far(what):
+    """For sizes (all of them or-ed together) with a bit past the 31 that the C entry takes; ctypes
+    would cut them."""
+    raise ValueError("%s must fit 32 bits" % what)
+
+
 def draft_tree(drafts, count, next_tok, nodes: int | None = None, eos: int = 0, out=None,
                stream=None):
     """Prefix tree of each query's drafts (Section 3.6), the tokens that one
@@ -449,6 +455,9 @@ def draft_tree(drafts, count, next_tok, nodes: int | None = None, eos: int = 0, 
     N = min(NODES_MAX, 1 + r * max(0, length - 1)) if nodes is None else int(nodes)
     if not 1 <= N <= NODES_MAX:
         raise ValueError("nodes must be in [1, %d]" % NODES_MAX)
+    eos = int(eos)
+    if (B | r | length) >> 31 or not -0x80000000 <= eos <= 0x7fffffff:
+        _too_far("the shape of drafts and eos")
     W = (N + 63) // 64
     with _on(stream, drafts, count, next_tok, *(out or ())):
         if out is None:
@@ -460,7 +469,7 @@ def draft_tree(drafts, count, next_tok, nodes: int | None = None, eos: int = 0, 
             _expect("mask", out[3], torch.int64, B, N, W)
             _expect("nodes", out[4], i32, B)
         _lib.check(_lib.load().dresd_draft_tree(
-            drafts.data_ptr(), count.data_ptr(), next_tok.data_ptr(), B, r, length, int(eos), N,
+            drafts.data_ptr(), count.data_ptr(), next_tok.data_ptr(), B, r, length, eos, N,
             *(t.data_ptr() for t in out), _current(drafts)))
     return tuple(out)
 
@@ -479,6 +488,8 @@ def _kv_cache(k_pages, v_pages, k_exp, v_exp):
     if code is None:
         raise TypeError("a cache is float16, bfloat16 or float8_e4m3fn, not %s" % k_pages.dtype)
     P, H, page, D = shape = _expect_dim("k_pages", k_pages, 4)
+    if (H | page | D) >> 31:
+        _too_far("a cache's heads, page size and dim")
     # (one condition where all is well: a call of one token is bound by these checks)
     if not (v_pages.dtype == k_pages.dtype and v_pages.shape == shape and k_pages.is_contiguous()
             and v_pages.is_contiguous()):
@@ -615,6 +626,8 @@ def paged_attention(q, k_pages, v_pages, table, lengths, starts=None, mask=None,
         if words < 1:          # (an empty tensor has no address, which is no mask)
             raise ValueError("mask must have a word a row at least")
         _expect("mask", mask, torch.int64, *q.shape[:-2], words)
+    if (n | B | H | width | words) >> 31:
+        _too_far("the shapes of q, table and mask")
     if scale is None:
         scale = cache.dim ** -0.5
     given = out if isinstance(out, (tuple, list)) else () if out is None else (out,)
@@ -662,6 +675,8 @@ def accept_drafts(logits, token, parent, nodes, most: int | None = None, out=Non
     _expect("parent", parent, i32, B, N)
     _expect("nodes", nodes, i32, B)
     most = N if most is None else int(most)
+    if (B | N | V | most) >> 31:
+        _too_far("the shape of logits and most")
     with _on(stream, logits, token, parent, nodes, *(out or ())):
         if out is None:
             out = (token.new_empty((B, most)), *token.new_empty((2, B)).unbind())

@@ -50,3 +50,40 @@ def test_a_mask_without_words():
     with pytest.raises(ValueError, match="word"):
         dresd.paged_attention(q.flatten(0, 1), kp, kp, table, lengths, starts=starts,
                               mask=mask.flatten(0, 1))
+
+
+FAR = (1 << 32) + 5            # 5 to who takes its lower 32 bits
+
+
+def far(*shape, dtype=torch.int32):
+    return torch.empty(*shape, dtype=dtype, device="meta")
+
+
+@pytest.mark.parametrize("call", [
+    lambda: dresd.draft_tree(far(1, FAR, 2), far(1), far(1), 8),
+    lambda: dresd.draft_tree(far(1, 2, FAR), far(1), far(1), 8),
+    lambda: dresd.draft_tree(far(FAR, 2, 3), far(FAR), far(FAR), 8),
+    lambda: dresd.draft_tree(far(1, 2, 3), far(1), far(1), 8, eos=FAR),
+    lambda: dresd.draft_tree(far(1, 2, 3), far(1), far(1), 8, eos=-(1 << 31) - 1),
+    lambda: dresd.accept_drafts(far(1, 1, FAR, dtype=torch.float16), far(1, 1), far(1, 1), far(1)),
+    lambda: dresd.accept_drafts(far(1, 2, 9, dtype=torch.float16), far(1, 2), far(1, 2), far(1), FAR),
+    lambda: dresd.accept_drafts(far(1, 2, 9, dtype=torch.float16), far(1, 2), far(1, 2), far(1), -1),
+    lambda: dresd.kv_read(far(1, dtype=torch.int64), *[far(1, 1, FAR, 8, dtype=torch.float16)] * 2),
+    lambda: dresd.kv_read(far(1, dtype=torch.int64), *[far(1, FAR, 1, 8, dtype=torch.float16)] * 2),
+    lambda: dresd.kv_read(far(1, dtype=torch.int64),
+                          *[far(1, 1, 1, (1 << 32) + 8, dtype=torch.float16)] * 2),
+    lambda: dresd.paged_attention(far(1, 1, 1, 8, dtype=torch.float16),
+                                  *[far(2, 1, 16, 8, dtype=torch.float16)] * 2, far(1, FAR), far(1)),
+    lambda: dresd.paged_attention(far(1, 1, 1, 8, dtype=torch.float16),
+                                  *[far(2, 1, 16, 8, dtype=torch.float16)] * 2, far(1, 3), far(1),
+                                  mask=far(1, 1, FAR, dtype=torch.int64)),
+    lambda: dresd.paged_attention(far(1, FAR, 8, dtype=torch.float16),
+                                  *[far(2, 1, 16, 8, dtype=torch.float16)] * 2, far(FAR, 3), far(FAR),
+                                  starts=far(FAR + 1)),
+    lambda: dresd.paged_attention(far(1, 1, FAR, 8, dtype=torch.float16),
+                                  *[far(2, 1, 16, 8, dtype=torch.float16)] * 2, far(1, 3), far(1)),
+], ids=range(15))
+def test_sizes_past_32_bits(call):
+    """The C entries take most sizes in 32 bits: what does not fit is refused, not cut."""
+    with pytest.raises(ValueError, match="32 bits"):
+        call()
