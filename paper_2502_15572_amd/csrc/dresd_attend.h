@@ -261,8 +261,9 @@ __device__ __forceinline__ bool unit_of(const AttendPlan &pl, Unit &u) {
   u.rows = u.n * pl.group;
   if (blk < 0 || blk > (u.rows - 1) / pl.rows) return false;  // (chunks that overlap)
   u.row0 = blk * pl.rows;
-  u.len = p.lengths[u.b];
-  u.before = (int64_t)u.len - u.n < -0x40000000 ? -0x40000000 : u.len - u.n;
+  const int len = p.lengths[u.b];
+  u.len = len > 0 ? len : 0;                 // (so that the tokens before the chunk stay inside 32 bits)
+  u.before = u.len - u.n;
   const int64_t room = (int64_t)p.width << p.c.page_log;
   u.L = u.len < room ? u.len : (int)room;
   u.L = u.L < kPositions ? u.L : kPositions;

@@ -67,3 +67,23 @@ def test_large_values_with_small_weights(gpu_lib, n, dim, dtype):
         assert (err <= tol).all()
         assert (np.abs(lse - wl) <= ds + 2.0 ** -20 + (L + 8) * 2.0 ** -24
                 + 2.0 ** -22 * np.abs(wl)).all()
+
+
+@pytest.mark.parametrize("length", [5, 0, -3, -(1 << 31)])
+def test_a_chunk_of_2_to_the_30_rows(gpu_lib, length):
+    """Of far fewer tokens than rows: the rows before the first position see nothing."""
+    from paper_2502_15572_amd import paged_attention
+    say("attend: 2^30 rows, length", length)
+    dev, n = "cuda:0", (1 << 30) + 200
+    x = torch.randn(3, 8, generator=torch.Generator().manual_seed(1)).to(torch.float16)
+    pages = torch.stack([x[0], x[1]]).view(2, 1, 1, 1, 8).expand(2, 1, 1, 16, 8).contiguous().to(dev)
+    q = x[2].to(dev).expand(1, n, 1, 8)
+    table = torch.zeros(1, 1, dtype=torch.int32, device=dev)
+    lengths = torch.tensor([length], dtype=torch.int32, device=dev)
+    out = torch.empty(1, n, 1, 8, dtype=torch.float16, device=dev)
+    out[0, -400:] = 7.0
+    paged_attention(q, pages[0], pages[1], table, lengths, out=out)
+    sees = max(0, length)                    # every key and value alike: the output is the value
+    last = out[0, -400:, 0].cpu()
+    assert (last[:400 - sees] == 0).all()
+    assert (last[400 - sees:] - x[1]).abs().le(2.0 ** -10 * x[1].abs()).all()
