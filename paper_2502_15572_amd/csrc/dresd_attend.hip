@@ -146,7 +146,7 @@ AttendPlan plan_of(const AttendParams &p, int cus) {
   // (464 units of up to 282 tokens on 512 places: two splits 20.9 us, one 15.1; drawn shapes 4 to 5%
   // on average).  Where one split leaves more than a quarter of the places empty, two, if the keys are
   // many (280 units of up to 12,000 tokens 190 us with one, 154 with two; 264 of 1,900 58
-  // with one, 64 with two).
+  // with one, 64 with two).  By the table's room: the lengths are on the device.
   const int64_t room = (int64_t)p.width << p.c.page_log;
   const int64_t slots = p.c.dim > 128 ? cus : 2 * (int64_t)cus;
   int64_t s = units > 0 ? slots / units : 1;

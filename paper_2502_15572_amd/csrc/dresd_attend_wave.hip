@@ -9,7 +9,7 @@
 // registers, past the caches and without a barrier; all slots but the one at hand are
 // on their way.  Page ids run one ring further ahead, as copies too, so that nothing
 // waits for memory but the wait for a whole tile.
-// 16-bit caches are read at 5.7 TB/s, 8-bit ones at 5.5 (64 sequences of 2,000 to 8,000 tokens,
+// 16-bit caches are read at 5.7 TB/s, 8-bit ones at 5.4 (64 sequences of 2,000 to 8,000 tokens,
 // 8 heads of 128, 8 query heads each); the copies alone, without the products,
 // reach 6.4 and 6.0, loads through the caches a tenth less.
 //

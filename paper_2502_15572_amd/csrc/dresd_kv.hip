@@ -15,7 +15,7 @@
 // lane carries 8 elements (16 bytes of a 16-bit row); the 8, 16 or 32 lanes of a row
 // find its largest magnitude by exchanges among them.  A write takes the key and
 // the value row of a token and head together: one look at the slot, two loads on their way
-// (16,384 tokens of 32 heads of 128, bf16 to 8 bits: 88 us, 4.6 TB/s of the 4.8 that a large
+// (16,384 tokens of 32 heads of 128, bf16 to 8 bits: 88 us a call, 4.6 TB/s of the 4.8 that a large
 // copy reaches; a row at a time 115).
 #include "dresd_device.h"
 #include "dresd_verify.h"
