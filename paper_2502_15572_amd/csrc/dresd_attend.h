@@ -305,7 +305,9 @@ __device__ __forceinline__ uint64_t window(const AttendPlan &pl, const Unit &u, 
   return w & (below(-j) | word(0) << (int)-j);
 }
 
-// out = x / l, lse = ref ln 2 + log l.
+// out = x / l, lse = (ref + log2 l) ln 2, where l's power of two and the reference, which may cancel
+// (f16 weights are kept at 2^10, those of 8-bit values at their values' power too), are joined
+// first, without a rounding larger than the result's.
 template <int QT>
 __device__ __forceinline__ void finish_row(const AttendParams &p, int64_t out, int d, f4 x,
                                            float ref, float l) {
@@ -315,8 +317,11 @@ __device__ __forceinline__ void finish_row(const AttendParams &p, int64_t out, i
 #pragma unroll
   for (int i = 0; i < 4; ++i) y[i] = __builtin_bit_cast(uint16_t, Half<QT>::round(x[i] * inv));
   *reinterpret_cast<us4 *>(static_cast<uint16_t *>(p.out) + out * p.c.dim + d) = y;
-  if (d == 0 && p.lse)
-    p.lse[out] = l != 0.f ? ref * 0.693147180559945309f + logf(l) : -__builtin_huge_valf();
+  if (d == 0 && p.lse) {
+    const float whole = ref + (float)__builtin_amdgcn_frexp_expf(l);
+    p.lse[out] = l != 0.f ? (whole + log2f(__builtin_amdgcn_frexp_mantf(l))) * 0.693147180559945309f
+                          : -__builtin_huge_valf();
+  }
 }
 
 // Four dims of a row of the output (head and row at `out` of [T, q_heads]): sums x

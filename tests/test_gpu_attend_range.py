@@ -87,3 +87,24 @@ def test_a_chunk_of_2_to_the_30_rows(gpu_lib, length):
     last = out[0, -400:, 0].cpu()
     assert (last[:400 - sees] == 0).all()
     assert (last[400 - sees:] - x[1]).abs().le(2.0 ** -10 * x[1].abs()).all()
+
+
+@pytest.mark.parametrize("dtype,cache", [("f16", "f8"), ("bf16", "f8"), ("f16", "f16")])
+@pytest.mark.parametrize("n,ctx", [(1, 1), (7, 1), (1, 900), (40, 3), (130, 70)])
+def test_logarithms_of_sums_near_the_reference(gpu_lib, n, ctx, dtype, cache):
+    """Scores of zero: a row's sum is the number of its positions, times a power of two that comes
+    from its values' size.  The weights and their sum are exact, the logarithm is off by two steps of
+    its fraction, of the sum with the exponent and of the product with ln 2."""
+    from paper_2502_15572_amd import paged_attention
+    say("attend: logarithms", n, ctx, dtype, cache)
+    for size in (0, 40, -40):
+        c = Case(n, [ctx], [n], 2, 3, 72, 16, dtype, cache)
+        if cache == "f8":
+            c.exp["v"] = np.where(c.exp["v"] == 255, 255, c.exp["v"].astype(np.int64)
+                                  + size).astype(np.uint8)
+        args, kw = c.tensors()
+        _, lse = paged_attention(*args, **kw, scale=0.0, with_lse=True)
+        want = np.log(ctx + 1.0 + np.arange(n))[:, None]
+        err = np.abs(lse.view(n, c.H).to(torch.float64).cpu().numpy() - want)
+        say("worst %.2e" % err.max())
+        assert (err <= 2.0 ** -22 * (1 + want)).all()
