@@ -262,7 +262,7 @@ __device__ __forceinline__ bool unit_of(const AttendPlan &pl, Unit &u) {
   if (blk < 0 || blk > (u.rows - 1) / pl.rows) return false;  // (chunks that overlap)
   u.row0 = blk * pl.rows;
   const int len = p.lengths[u.b];
-  u.len = len > 0 ? len : 0;                 // (so that the tokens before the chunk stay inside 32 bits)
+  u.len = len > 0 ? len : 0;                 // (so that the difference stays inside 32 bits)
   u.before = u.len - u.n;
   const int64_t room = (int64_t)p.width << p.c.page_log;
   u.L = u.len < room ? u.len : (int)room;

@@ -2,13 +2,14 @@
 // heads of one cache head) a workgroup, 32 a wave.
 //
 // What bounds it is the matrix cores, and beside them the exponentials: 128 rows do 128
-// multiply-adds per 16-bit value read (busy 46% and 45% of the time, LDS 27%: a wave's products and
-// exponentials follow one another, two waves a SIMD overlap them).  The four waves share each tile of 64 keys and
-// values through LDS, two tiles deep: while one is computed the next is copied to the
-// other buffer (8-bit rows through registers, where they are converted, once for all four
-// waves), and a tile has one barrier.  A chunk of 2,048 tokens over 16,000 and two shorter
-// ones (8 x 4 heads of 128, bf16): 1.16 to 1.22 ms by card, 910 to 960 TFLOP/s, where a
-// 16,384^3 product of the library reaches 1,374; rows through registers took 0.13 ms more.
+// multiply-adds per 16-bit value read (busy 46% and 45% of the time, LDS 27%: a wave's products
+// and exponentials follow one another, and two waves a SIMD overlap theirs).  The four waves
+// share each tile of 64 keys and values through LDS, two tiles deep: while one is computed the
+// next is copied to the other buffer (8-bit rows through registers, where they are converted,
+// once for all four waves), and a tile has one barrier.  A chunk of 2,048 tokens over 16,000 and
+// two shorter ones (8 x 4 heads of 128, bf16): 1.16 to 1.22 ms by card, 910 to 960 TFLOP/s,
+// where a 16,384^3 product of the library reaches 1,374; rows through registers took 0.13 ms
+// more.
 //
 // Scores are formed transposed, S^T = K Q^T, with 32 x 32 x 16 instructions: a lane
 // holds one row (lane % 32) and half the keys, which is, keys in another order, the
